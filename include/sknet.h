@@ -370,6 +370,71 @@ sk_status sknet3d_get_weights(sknet3d_t *net, int32_t conv_idx, float *w_host, f
 sk_status sknet3d_get_activation(sknet3d_t *net, int32_t layer_idx, float *dchw_host);
 sk_status sknet3d_get_pool_argmax(sknet3d_t *net, int32_t pool_idx, int32_t *idx_host);
 
+/* ---------------------------------------------------------------- operators on the caller's own tensors */
+
+/* Dropout and layer norm over the channels (maps) of each position, forwards and backwards, on tensors that the caller owns.
+ *
+ * A tensor has n * plane positions of c >= 1 channels in one of two orders:
+ *   SK_ROWS: channel k of row r is element r*stride_n + k; plane must be 1 and stride_c is ignored;
+ *   SK_MAPS: channel k of pixel m of image b is element b*stride_n + k*stride_c + m (planes of pixels, as the maps of a net).
+ * Position number: b*plane + m.  Strides count elements and may be larger than a dense tensor's; inputs may have strides of 0,
+ * elements of an output must not share a place.  dtype is the type of every sk_view of a call; parameters, statistics and
+ * parameter gradients are fp32, and so is everything in between: 16-bit values are rounded when they are stored, once.
+ * Data need no alignment beyond their elements'.  n or plane of 0 is allowed (the views' data may then be NULL): nothing runs but the clearing of
+ * parameter gradients.  Limits (SK_EUNSUPPORTED): 2^27 channels, 2^40 positions, 2^46 elements reached.
+ *
+ * In place: an output may be the tensor of an input, with the same strides.  SK_EINVAL for any other overlap of an output
+ * with an input or another output, as far as views of one call go.
+ *
+ * Everything is enqueued on hip_stream; the current HIP device must be that of the stream and the buffers.  Nothing is
+ * allocated, kept or synchronised: calls can be recorded into a graph, and may overlap as long as their buffers do not. */
+typedef enum { SK_ROWS = 0, SK_MAPS = 1 } sk_layout;
+typedef struct {
+    int32_t dtype;  /* sk_dtype */
+    int32_t layout; /* sk_layout */
+    int64_t n, c, plane;
+} sk_extent;
+typedef struct {
+    void *data; /* DEVICE */
+    int64_t stride_n, stride_c;
+} sk_view;
+
+/* A dropout mask.  It is never stored: the 16-bit number of channel k of position q is half-word k mod 8 (low half of a word first) of the four words
+ * that Philox4x32-10 (Salmon et al., Parallel random numbers: as easy as 1, 2, 3, SC 2011) makes of the key `seed` and the
+ * counter words {q mod 2^32, k / 8 + 2^24 (q / 2^32), o mod 2^32, o / 2^32}, o = offset + *step_dev; an element is kept if its number is
+ * at least t = floor(65536 p + 1/2), and then scaled by 65536 / (65536 - t).  So the mask depends on the seed, the offset and the logical place
+ * alone, not on type, order or strides, and the backward pass makes the forward pass's mask again from the same sk_drop.
+ * Dropped elements are 0 (NaN and infinite ones too).  p in [0, 1].  step_dev: DEVICE, 8-byte aligned, or NULL (= 0): a counter that a recorded
+ * graph advances between its replays; forward and backward must see the same value. */
+typedef struct {
+    double p;
+    uint64_t seed, offset;
+    const uint64_t *step_dev;
+} sk_drop;
+
+/* y = dropout(x).  The gradient of x is the same call on the gradient of y. */
+sk_status sknet_dropout(const sk_extent *extent, const sk_view *x, const sk_view *y, const sk_drop *drop, void *hip_stream);
+
+/* s = residual + dropout(x) (residual, drop: NULL leaves either out);  per position: mean = sum_k s / c,
+ * rstd = 1 / sqrt(sum_k (s - mean)^2 / c + eps);  y = (s - mean) * rstd * gamma + beta.
+ * gamma_dev, beta_dev: DEVICE [c], NULL = 1 and 0.  sum (NULL: not stored) receives s; y is made from s before that is rounded.  mean_dev, rstd_dev:
+ * DEVICE [n*plane], NULL = not stored.  eps > 0. */
+sk_status sknet_layer_norm(const sk_extent *extent, const sk_view *x, const sk_view *residual, const sk_drop *drop, const float *gamma_dev,
+                           const float *beta_dev, float eps, const sk_view *sum, const sk_view *y, float *mean_dev, float *rstd_dev,
+                           void *hip_stream);
+
+/* Gradients of sknet_layer_norm.  s: what was normalised (the forward call's sum, or its x if nothing was added to x); with
+ * h = (s - mean) * rstd and g = gamma * dy:
+ *   t = rstd * (g - sum_k g / c - h * sum_k(g h) / c) + dsum;  dresidual = t;  dx = dropout(t);
+ *   dgamma = sum over positions of dy h;  dbeta = sum over positions of dy.
+ * dsum: the gradient that reaches s from elsewhere, or NULL.  drop: the forward call's, or NULL.  dx, dresidual, dgamma_dev, dbeta_dev: each may
+ * be NULL.  Sums are taken in a fixed order: equal calls give equal bits.  workspace_dev: DEVICE, 16-byte aligned, of at least
+ * the bytes that sknet_layer_norm_workspace reports for the extent (NULL if neither dgamma nor dbeta is asked for), used until the call's work has run. */
+sk_status sknet_layer_norm_workspace(const sk_extent *extent, uint64_t *bytes);
+sk_status sknet_layer_norm_backward(const sk_extent *extent, const sk_view *dy, const sk_view *s, const float *mean_dev, const float *rstd_dev,
+                                    const float *gamma_dev, const sk_view *dsum, const sk_drop *drop, const sk_view *dx, const sk_view *dresidual,
+                                    float *dgamma_dev, float *dbeta_dev, void *workspace_dev, uint64_t workspace_bytes, void *hip_stream);
+
 /* Machine probes for the benchmark (Section 6 of the paper times kernels against each device's
  * peak; these two calls measure the peaks of the device at hand).  Neither runs any step of the method.
  *

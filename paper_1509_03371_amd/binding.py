@@ -4,6 +4,7 @@ step of the path runs inside the library's HIP kernels.  There is no CPU fallbac
 is missing, importing this module raises.
 """
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -18,6 +19,7 @@ lib = C.CDLL(LIB_PATH)
 
 SK_F32, SK_BF16, SK_F16 = 0, 1, 2
 SK_CONV, SK_MAXPOOL = 0, 1
+SK_ROWS, SK_MAPS = 0, 1
 STATUS_NAMES = ["SK_OK", "SK_EINVAL", "SK_ESHAPE", "SK_ESTATE", "SK_ENOMEM", "SK_EDEVICE", "SK_EUNSUPPORTED"]
 DTYPES = {"f32": SK_F32, "bf16": SK_BF16, "f16": SK_F16}
 
@@ -30,6 +32,18 @@ class SkLayer(C.Structure):
 class SwLayer(C.Structure):
     _fields_ = [("kind", C.c_int32), ("c_out", C.c_int32), ("k", C.c_int32), ("s", C.c_int32),
                 ("relu", C.c_int32)]
+
+
+class SkExtent(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("layout", C.c_int32), ("n", C.c_int64), ("c", C.c_int64), ("plane", C.c_int64)]
+
+
+class SkView(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_n", C.c_int64), ("stride_c", C.c_int64)]
+
+
+class SkDrop(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64), ("step_dev", C.c_void_p)]
 
 
 class SknetError(RuntimeError):
@@ -93,6 +107,10 @@ _SIGS = {
     "sknet3d_get_grad": [_vp, _i32, _fp, _fp],
     "sknet3d_get_weights": [_vp, _i32, _fp, _fp],
     "sknet3d_get_pool_argmax": [_vp, _i32, _ip],
+    "sknet_dropout": [_vp, _vp, _vp, _vp, _vp],
+    "sknet_layer_norm": [_vp, _vp, _vp, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp, _vp, _vp],
+    "sknet_layer_norm_workspace": [_vp, C.POINTER(C.c_uint64)],
+    "sknet_layer_norm_backward": [_vp] * 13 + [C.c_uint64, _vp],
     "sk_probe_mfma": [_i32, _i32, _i32, _vp, C.POINTER(C.c_double)],
     "sk_probe_copy": [_vp, _vp, C.c_uint64, _i32, _vp, C.POINTER(C.c_double)],
     "sk_probe_conv_path": [_i32] * 8 + [_ip],
@@ -206,6 +224,194 @@ def sknet_convert_sw(sw_layers, w0_sw):
         else:
             res.append({"type": "pool", "k": l.k, "d": l.d, "s": l.s})
     return res
+
+
+# ---- operators on the caller's own tensors ------------------------------------------------------------------------
+
+_OP_TYPES = {torch.float32: SK_F32, torch.bfloat16: SK_BF16, torch.float16: SK_F16}
+
+
+@functools.lru_cache(maxsize=4096)
+def _orders(shape, strides, axis):
+    """{(layout, n, c, plane): (stride_n, stride_c)}: every way to see a tensor of these sizes and strides with its channels on
+    `axis` as rows or as maps, rows and the largest planes first.  Positions count in the order of the other axes."""
+    others = [(shape[a], strides[a]) for a in range(len(shape)) if a != axis]
+    c, sc = shape[axis], strides[axis]
+
+    def merged(parts):                             # axes as one: (length, stride), None if their strides do not allow it
+        length, stride = 1, 0
+        for size, step in reversed(parts):
+            if size == 1:
+                continue
+            if length == 1:
+                stride = step
+            elif step != stride * length:
+                return None
+            length *= size
+        return length, stride
+
+    if any(size == 0 for size, _ in others):
+        return {(SK_ROWS, 0, c, 1): (0, 0)}
+    found = {}
+    rows = merged(others) if c == 1 or sc == 1 else None
+    if rows is not None:
+        found[SK_ROWS, rows[0], c, 1] = rows[1], 0
+    for cut in range(len(others) + 1):             # the axes from `cut` on are the plane
+        outer, inner = merged(others[:cut]), merged(others[cut:])
+        if outer is not None and inner is not None and (inner[0] == 1 or inner[1] == 1):
+            found.setdefault((SK_MAPS, outer[0], c, inner[0]), (outer[1], sc))
+    return found
+
+
+class _Operator:
+    """One call of an operator: its stream and device, and its tensors as views of one extent."""
+
+    def __init__(self, x, axis, what, stream):
+        if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype in _OP_TYPES):
+            raise TypeError("%s must be a CUDA tensor of float32, bfloat16 or float16" % what)
+        if not -x.dim() <= axis < x.dim():
+            raise ValueError("%s has no axis %d" % (what, axis))
+        self.x, self.what, self.axis, self.device = x, what, axis % x.dim(), x.device
+        self.views = {}
+        current = torch.cuda.current_stream(x.device)
+        self.scope = None
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=x.device)
+        if stream is None:
+            stream = current
+        elif stream.device != x.device:
+            raise ValueError("the stream is not one of %s" % (x.device,))
+        # the call runs, and what it allocates belongs, there
+        if stream.cuda_stream != current.cuda_stream or x.device.index != torch.cuda.current_device():
+            self.scope = torch.cuda.stream(stream)
+        self.stream = C.c_void_p(stream.cuda_stream)
+
+    def __enter__(self):
+        if self.scope is not None:
+            self.scope.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+
+    def output(self):
+        """A tensor for a result: x's sizes and order of axes, without its gaps."""
+        return torch.empty_like(self.x, memory_format=torch.contiguous_format if self.x.is_contiguous() else torch.preserve_format)
+
+    def place(self, **tensors):
+        """Find the order that the tensors have in common; returns the extent, and their views by name (None for None)."""
+        x, axis = self.x, self.axis
+        choices = _orders(x.shape, x.stride(), axis)
+        theirs = {}
+        for name, t in tensors.items():
+            if t is None or t is x:
+                continue
+            if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == x.dtype):
+                raise TypeError("%s must be a tensor of %s on %s" % (name, x.dtype, self.device))
+            if t.shape != x.shape:
+                raise ValueError("%s has shape %s instead of %s" % (name, tuple(t.shape), tuple(x.shape)))
+            theirs[name] = _orders(t.shape, t.stride(), axis)
+        for order in choices:
+            if all(order in o for o in theirs.values()):
+                break
+        else:
+            raise ValueError("%s, strides %s, keep the channels of axis %d neither as rows nor as maps in common; make them contiguous" % (
+                ", ".join([self.what] + sorted(theirs)), [x.stride()] + [tensors[n].stride() for n in sorted(theirs)], axis))
+        layout, n, c, plane = order
+        self.order = order
+        self.extent = SkExtent(_OP_TYPES[x.dtype], layout, n, c, plane)
+        out = [SkView(x.data_ptr(), *choices[order])]
+        for name, t in tensors.items():
+            out.append(None if t is None else out[0] if t is x else SkView(t.data_ptr(), *theirs[name][order]))
+        self.held = out
+        return [None if v is None else C.byref(v) for v in out]
+
+    def values(self, t, count, name):
+        """DEVICE pointer of `count` fp32 values, None for None."""
+        if t is None:
+            return None
+        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == torch.float32 and t.is_contiguous()):
+            raise TypeError("%s must be a contiguous tensor of torch.float32 on %s" % (name, self.device))
+        if t.numel() != count:
+            raise ValueError("%s has %d values instead of %d" % (name, t.numel(), count))
+        return t.data_ptr()
+
+    def drop(self, p, seed, offset, step):
+        if step is not None and not (isinstance(step, torch.Tensor) and step.device == self.device and step.dtype == torch.int64 and step.numel() == 1):
+            raise TypeError("step must be one value of torch.int64 on %s" % (self.device,))
+        if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+            raise ValueError("seed and offset are unsigned 64-bit numbers")
+        return C.byref(SkDrop(p, seed, offset, None if step is None else step.data_ptr()))
+
+
+def dropout(x, p, seed, offset=0, axis=-1, out=None, step=None, stream=None):
+    """x with the elements of the mask (seed, offset + step, p) zeroed and the others scaled; the gradient of x is the same call on
+    the gradient of the result.  axis: the channels'; the mask belongs to the (position, channel) of an element, whatever the strides.  step:
+    optional tensor of one int64, read when the call runs (a recorded graph can advance it)."""
+    with _Operator(x, axis, "x", stream) as op:
+        if out is None:
+            out = op.output()
+        xv, yv = op.place(out=out)
+        _check(lib.sknet_dropout(C.byref(op.extent), xv, yv, op.drop(p, seed, offset, step), op.stream))
+    return out
+
+
+def layer_norm(x, gamma=None, beta=None, eps=1e-5, axis=-1, residual=None, p=0.0, seed=0, offset=0, step=None, out=None, sum_out=None, mean=None,
+               rstd=None, stream=None):
+    """(y, s, mean, rstd): y = (s - mean) * rstd * gamma + beta with the mean and 1 / sqrt(variance + eps) of s = residual +
+    dropout(x) over the channels on `axis`.  s is x itself where nothing is added or dropped (p = 0); mean and rstd have x's axes without
+    the channels'.  out, sum_out, mean, rstd: tensors to write to."""
+    with _Operator(x, axis, "x", stream) as op:
+        plain = residual is None and p == 0.0 and sum_out is None
+        if out is None:
+            out = op.output()
+        if sum_out is None and not plain:
+            sum_out = op.output()
+        if mean is None or rstd is None:
+            shape = x.shape[:op.axis] + x.shape[op.axis + 1:]
+            mean = torch.empty(shape, dtype=torch.float32, device=x.device) if mean is None else mean
+            rstd = torch.empty(shape, dtype=torch.float32, device=x.device) if rstd is None else rstd
+        xv, rv, sv, yv = op.place(residual=residual, sum_out=sum_out, out=out)
+        _, n, c, plane = op.order
+        drop = None if p == 0.0 else op.drop(p, seed, offset, step)
+        _check(lib.sknet_layer_norm(C.byref(op.extent), xv, rv, drop, op.values(gamma, c, "gamma"), op.values(beta, c, "beta"), eps, sv, yv,
+                                    op.values(mean, n * plane, "mean"), op.values(rstd, n * plane, "rstd"), op.stream))
+    return out, x if plain else sum_out, mean, rstd
+
+
+def layer_norm_backward(dy, s, mean, rstd, gamma=None, axis=-1, dsum=None, p=0.0, seed=0, offset=0, step=None, residual=True, parameters=True,
+                        dx=None, dresidual=None, dgamma=None, dbeta=None, stream=None):
+    """(dx, dresidual, dgamma, dbeta) of layer_norm's y, with the s, mean, rstd it returned and its p, seed, offset and step.  dsum: the gradient that
+    reaches s from elsewhere.  dresidual is the gradient of s, and dx dropout of it: one tensor if p = 0 (then leave
+    dresidual out).  residual=False: no dresidual (None) where p > 0; parameters=False: no dgamma and dbeta (None)."""
+    with _Operator(dy, axis, "dy", stream) as op:
+        if dx is None:
+            dx = op.output()
+        if p == 0.0:
+            if dresidual is not None and dresidual is not dx:
+                raise ValueError("without dropout dx is the gradient of the residual too; leave dresidual out")
+            dresidual = None
+        elif dresidual is None and residual:
+            dresidual = op.output()
+        dyv, sv, dsv, dxv, drv = op.place(s=s, dsum=dsum, dx=dx, dresidual=dresidual)
+        _, n, c, plane = op.order
+        workspace, bytes_ = None, 0
+        if parameters:
+            dgamma = torch.empty(c, dtype=torch.float32, device=dy.device) if dgamma is None else dgamma
+            dbeta = torch.empty(c, dtype=torch.float32, device=dy.device) if dbeta is None else dbeta
+            need = C.c_uint64()
+            _check(lib.sknet_layer_norm_workspace(C.byref(op.extent), C.byref(need)))
+            bytes_ = need.value
+            if bytes_:
+                workspace = torch.empty(bytes_, dtype=torch.uint8, device=dy.device)
+        elif dgamma is not None or dbeta is not None:
+            raise ValueError("parameters=False leaves no gradients to write")
+        drop = None if p == 0.0 else op.drop(p, seed, offset, step)
+        _check(lib.sknet_layer_norm_backward(C.byref(op.extent), dyv, sv, op.values(mean, n * plane, "mean"), op.values(rstd, n * plane, "rstd"),
+                                             op.values(gamma, c, "gamma"), dsv, drop, dxv, drv, op.values(dgamma, c, "dgamma"),
+                                             op.values(dbeta, c, "dbeta"), None if workspace is None else workspace.data_ptr(), bytes_, op.stream))
+    return dx, dx if p == 0.0 else dresidual, dgamma, dbeta
 
 
 class SKNet:
