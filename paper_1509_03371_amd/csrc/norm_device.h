@@ -1,0 +1,101 @@
+// Loads, stores and sums shared by the norm and dropout kernels (internal device code).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "norm.h"
+
+namespace sk {
+
+template <int DT> struct Elem;
+template <> struct Elem<0> { typedef float type; };
+template <> struct Elem<1> { typedef __bf16 type; };
+template <> struct Elem<2> { typedef _Float16 type; };
+template <int DT> using elem_t = typename Elem<DT>::type;
+
+// N elements side by side, aligned to one element only: the hardware takes global accesses of four words at any
+// address, and rows or planes of odd length begin anywhere
+template <int DT, int N> struct Line {
+    typedef elem_t<DT> type __attribute__((ext_vector_type(N), aligned(sizeof(elem_t<DT>))));
+};
+template <int DT, int N> using line_t = typename Line<DT, N>::type;
+
+// elements first .. first + N - 1 of a line of `count`; zeros where it has none
+template <int DT, int N> __device__ __forceinline__ line_t<DT, N> load_line(const elem_t<DT> *p, long first, long count)
+{
+    line_t<DT, N> v;
+    if (first + N <= count) return *reinterpret_cast<const line_t<DT, N> *>(p + first);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = first + j < count ? p[first + j] : static_cast<elem_t<DT>>(0.f);
+    return v;
+}
+
+template <int DT, int N> __device__ __forceinline__ void store_line(elem_t<DT> *p, long first, long count, const float (&f)[N])
+{
+    if (first + N <= count) {
+        line_t<DT, N> v;
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = static_cast<elem_t<DT>>(f[j]);
+        *reinterpret_cast<line_t<DT, N> *>(p + first) = v;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (first + j < count) p[first + j] = static_cast<elem_t<DT>>(f[j]);
+}
+
+// v + the v of the lane whose number differs in bit STEP, over lanes whose lower bits are summed already (STEP 4 and 8: mirrored
+// halves, of which every lane of a half holds the same); exchanges within sixteen lanes are operand modifiers, not LDS traffic
+template <int STEP> __device__ __forceinline__ float add_across(float v)
+{
+    if (STEP == 1) return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xF, 0xF, true));      // lanes 1 0 3 2 of four
+    if (STEP == 2) return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xF, 0xF, true));      // lanes 2 3 0 1 of four
+    if (STEP == 4) return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xF, 0xF, true));     // eight lanes mirrored
+    if (STEP == 8) return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xF, 0xF, true));     // sixteen lanes mirrored
+    return v + __shfl_xor(v, STEP);
+}
+
+// sum over groups of G neighbouring lanes (G a power of two up to 64), in every lane of the group
+template <int G> __device__ __forceinline__ float sum_lanes(float v)
+{
+    if (G > 1) v = add_across<1>(v);
+    if (G > 2) v = add_across<2>(v);
+    if (G > 4) v = add_across<4>(v);
+    if (G > 8) v = add_across<8>(v);
+    if (G > 16) v = add_across<16>(v);
+    if (G > 32) v = add_across<32>(v);
+    return v;
+}
+
+// sum over the lanes with equal number modulo P (P a power of two from 4 to 64), in every one of them
+template <int P> __device__ __forceinline__ float sum_over_groups(float v)
+{
+    if (P < 8) v += __shfl_xor(v, 4);
+    if (P < 16) v += __shfl_xor(v, 8);
+    if (P < 32) v += __shfl_xor(v, 16);
+    if (P < 64) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// workgroups for so much work: up to 2^21 (a grid may have 2^32 - 1 threads), which then walk it
+inline unsigned norm_blocks(long work, long each)
+{
+    const long b = (work + each - 1) / each;
+    return (unsigned)(b < (1L << 21) ? b : 1L << 21);
+}
+
+// dgamma and dbeta from the `copies` copies of their sums, each [2][c rounded up to 4]
+hipError_t launch_norm_reduce(const float *scratch, int copies, float *dgamma, float *dbeta, int c, hipStream_t stream);
+__host__ __device__ inline long norm_copy_floats(long c) { return 2 * ((c + 3) / 4 * 4); }
+
+// the kernels for each order of the channels
+hipError_t launch_norm_rows(const NormArgs &a, hipStream_t stream);
+hipError_t launch_norm_planes(const NormArgs &a, hipStream_t stream);          // MAPS and OCTETS
+int norm_rows_bwd_copies(const NormSpan &s);
+int norm_planes_bwd_copies(const NormSpan &s);
+hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t stream);
+hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t stream);
+
+}  // namespace sk
