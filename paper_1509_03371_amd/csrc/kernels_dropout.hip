@@ -5,61 +5,80 @@ namespace sk {
 
 namespace {
 
-// A thread takes the eight channels of an octet that one call of the generator serves; bx (a power of two) octets of a row lie side by side
-// in a workgroup.
+// A thread takes the eight channels of an octet that one call of the generator serves; 1 << shift octets of a row lie side by side in a workgroup.
 template <int DT> __global__ __launch_bounds__(256) void dropout_rows_kernel(DropoutArgs a, int shift, int parts)
 {
     typedef elem_t<DT> E;
-    const uint64_t base = a.drop.base();
-    const int across = 1 << shift, down = 256 >> shift;
-    const int o = (blockIdx.x % parts) * across + (threadIdx.x & (across - 1));
-    if (8 * o >= a.c) return;
+    const uint64_t counter = a.drop.base();
+    const int down = 256 >> shift, c0 = 8 * (((blockIdx.x % parts) << shift) + (threadIdx.x & ((1 << shift) - 1))), left = a.c - c0;
+    if (left <= 0) return;
     const long step = gridDim.x / parts * (long)down;
     for (long row = blockIdx.x / parts * (long)down + (threadIdx.x >> shift); row < a.n; row += step) {
-        const line_t<DT, 8> x = load_line<DT, 8>(static_cast<const E *>(a.x.p) + row * a.x.sn, 8 * o, a.c);
+        const E *x = static_cast<const E *>(a.x.p) + row * a.x.sn + c0;
+        E *y = static_cast<E *>(a.y.p) + row * a.y.sn + c0;
         uint32_t w[4];
-        mask_words(w, a.drop, base, (uint64_t)row, o);
-        float y[8];
+        if (left >= 8) {
+            Words<DT, 8> v;
+            v.load(reinterpret_cast<src_t>(x), 0);
+            mask_words(w, a.drop, counter, (uint64_t)row, c0 / 8);
+            float f[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = dropped((float)x[j], w, j, a.drop);
-        store_line<DT, 8>(static_cast<E *>(a.y.p) + row * a.y.sn, 8 * o, a.c, y);
+            for (int j = 0; j < 8; ++j) f[j] = dropped(v[j], w, j, a.drop);
+            store_at<DT, 8>(reinterpret_cast<dst_t>(y), 0, f);
+        } else {
+            mask_words(w, a.drop, counter, (uint64_t)row, c0 / 8);
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < left) y[j] = static_cast<E>(dropped((float)x[j], w, j, a.drop));
+        }
     }
 }
 
-// Maps: a thread takes an octet of channels of four pixels side by side.
-template <int DT> __global__ __launch_bounds__(256) void dropout_maps_kernel(DropoutArgs a, long tiles, int octs, long parts)
+// Maps: a thread takes an octet of channels of V pixels side by side.  Lanes whose pixels would reach over the plane's end take its last V instead (those
+// that two lanes of a wave then hold are computed alike and stored twice, after both have read).
+template <int DT, int V> __global__ __launch_bounds__(256) void dropout_maps_kernel(DropoutArgs a, long tiles, int octs, long parts)
 {
     typedef elem_t<DT> E;
-    constexpr int V = 4;
-    const uint64_t base = a.drop.base();
+    const uint64_t counter = a.drop.base();
     for (long t = blockIdx.x; t < tiles; t += gridDim.x) {          // tile: (image, octet, part of the plane), the last fastest
-        const long line = t / parts, b = line / octs, pixel = (t % parts * 256L + threadIdx.x) * V;
-        const int o = (int)(line % octs);
-        if (pixel >= a.plane) continue;
-        const E *x = static_cast<const E *>(a.x.p) + b * a.x.sn + 8L * o * a.x.sc;
-        E *y = static_cast<E *>(a.y.p) + b * a.y.sn + 8L * o * a.y.sc;
-        line_t<DT, V> v[8];
+        const long line = t / parts, b = line / octs, first = t % parts * 256L * V, begin = first + threadIdx.x * V;
+        const int o = (int)(line % octs), left = a.c - 8 * o;
+        if (begin >= a.plane) continue;
+        const long from = first < a.plane - V ? first : a.plane - V;
+        const uint32_t px = (uint32_t)((begin < a.plane - V ? begin : a.plane - V) - from), off = px * sizeof(E);
+        src_t x = reinterpret_cast<src_t>(static_cast<const E *>(a.x.p) + b * a.x.sn + 8L * o * a.x.sc + from);
+        dst_t y = reinterpret_cast<dst_t>(static_cast<E *>(a.y.p) + b * a.y.sn + 8L * o * a.y.sc + from);
+        const long up_x = a.x.sc * sizeof(E), up_y = a.y.sc * sizeof(E), up_r = a.relu_src.sc * sizeof(E);
+        Words<DT, V> v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 8 * o + j < a.c ? load_line<DT, V>(x + j * a.x.sc, pixel, a.plane) : line_t<DT, V>{};
-        float f[8][V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            uint32_t w[4];
-            mask_words(w, a.drop, base, (uint64_t)(b * a.plane + pixel + i), o);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j][i] = dropped((float)v[j][i], w, j, a.drop);
-        }
-        const E *r = static_cast<const E *>(a.relu_src.p) + b * a.relu_src.sn + 8L * o * a.relu_src.sc;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (8 * o + j >= a.c) break;
-            if (a.relu_src.p) {
-                const line_t<DT, V> u = load_line<DT, V>(r + j * a.relu_src.sc, pixel, a.plane);
-#pragma unroll
-                for (int i = 0; i < V; ++i) f[j][i] = (float)u[i] > 0.f ? f[j][i] : 0.f;
+        for (int j = 0; j < 8; ++j) v[j].load(x + std::min(j, left - 1) * up_x, off);        // (channels behind the last repeat it)
+        uint32_t bits = 0;
+        auto draw = [&](auto i) {
+            if constexpr (i() < V) {
+                uint32_t w[4];
+                mask_words(w, a.drop, counter, (uint64_t)(b * a.plane + from + px + i()), o);
+                bits |= keep_bits<8 * i()>(w, a.drop);
             }
-            store_line<DT, V>(y + j * a.y.sc, pixel, a.plane, f[j]);
-        }
+        };
+        draw(std::integral_constant<int, 0>{});
+        draw(std::integral_constant<int, 1>{});
+        draw(std::integral_constant<int, 2>{});
+        draw(std::integral_constant<int, 3>{});
+        src_t r = reinterpret_cast<src_t>(static_cast<const E *>(a.relu_src.p) + b * a.relu_src.sn + 8L * o * a.relu_src.sc + from);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left) {
+                float f[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] = kept(v[j][i], bits, 8 * i + j, a.drop);
+                if (a.relu_src.p) {
+                    Words<DT, V> u;
+                    u.load(r + j * up_r, off);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) f[i] = u[i] > 0.f ? f[i] : 0.f;
+                }
+                store_at<DT, V>(y + j * up_y, off, f);
+            }
     }
 }
 
@@ -67,24 +86,24 @@ template <int DT> __global__ __launch_bounds__(256) void dropout_maps_kernel(Dro
 template <int DT> __global__ __launch_bounds__(256) void dropout_octets_kernel(DropoutArgs a, long tiles, int octs, long parts)
 {
     typedef elem_t<DT> E;
-    const uint64_t base = a.drop.base();
+    const uint64_t counter = a.drop.base();
     for (long t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const long line = t / parts, b = line / octs, pixel = t % parts * 256L + threadIdx.x;
-        const int o = (int)(line % octs);
-        if (pixel >= a.plane) continue;
-        const line_t<DT, 8> x = *reinterpret_cast<const line_t<DT, 8> *>(static_cast<const E *>(a.x.p) + b * a.x.sn + o * a.x.sc + 8 * pixel);
-        line_t<DT, 8> r{};
-        if (a.relu_src.p) r = *reinterpret_cast<const line_t<DT, 8> *>(static_cast<const E *>(a.relu_src.p) + b * a.relu_src.sn + o * a.relu_src.sc + 8 * pixel);
+        const long line = t / parts, b = line / octs, first = t % parts * 256L;
+        const int o = (int)(line % octs), left = a.c - 8 * o;
+        if (first + threadIdx.x >= a.plane) continue;
+        const uint32_t off = threadIdx.x * 8 * sizeof(E);
+        Words<DT, 8> x, r;
+        x.load(reinterpret_cast<src_t>(static_cast<const E *>(a.x.p) + b * a.x.sn + o * a.x.sc + 8 * first), off);
+        if (a.relu_src.p) r.load(reinterpret_cast<src_t>(static_cast<const E *>(a.relu_src.p) + b * a.relu_src.sn + o * a.relu_src.sc + 8 * first), off);
         uint32_t w[4];
-        mask_words(w, a.drop, base, (uint64_t)(b * a.plane + pixel), o);
-        line_t<DT, 8> y;
+        mask_words(w, a.drop, counter, (uint64_t)(b * a.plane + first + threadIdx.x), o);
+        float y[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float v = dropped((float)x[j], w, j, a.drop);
-            if (8 * o + j >= a.c || (a.relu_src.p && !((float)r[j] > 0.f))) v = 0.f;
-            y[j] = static_cast<E>(v);
+            y[j] = dropped(x[j], w, j, a.drop);
+            if (j >= left || (a.relu_src.p && !(r[j] > 0.f))) y[j] = 0.f;
         }
-        *reinterpret_cast<line_t<DT, 8> *>(static_cast<E *>(a.y.p) + b * a.y.sn + o * a.y.sc + 8 * pixel) = y;
+        store_at<DT, 8>(reinterpret_cast<dst_t>(static_cast<E *>(a.y.p) + b * a.y.sn + o * a.y.sc + 8 * first), off, y);
     }
 }
 
@@ -103,10 +122,11 @@ template <int DT> hipError_t launch(const DropoutArgs &a, hipStream_t stream)
         const long most = std::max(1L, (1L << 21) / parts);
         dropout_rows_kernel<DT><<<(unsigned)(std::min(rows, most) * parts), 256, 0, stream>>>(a, shift, parts);
     } else {
-        const int pixels = a.layout == MAPS ? 1024 : 256;
-        const long parts = (a.plane + pixels - 1) / pixels, tiles = a.n * octs * parts;
-        if (a.layout == MAPS) dropout_maps_kernel<DT><<<norm_blocks(tiles, 1), 256, 0, stream>>>(a, tiles, octs, parts);
-        else if (DT != 0) dropout_octets_kernel<DT><<<norm_blocks(tiles, 1), 256, 0, stream>>>(a, tiles, octs, parts);
+        const int v = a.layout == MAPS && a.plane >= 4 ? 4 : 1;
+        const long parts = (a.plane + 256 * v - 1) / (256 * v), tiles = a.n * octs * parts;
+        if (a.layout == MAPS && v == 4) dropout_maps_kernel<DT, 4><<<norm_blocks(tiles, 1), 256, 0, stream>>>(a, tiles, octs, parts);
+        else if (a.layout == MAPS) dropout_maps_kernel<DT, 1><<<norm_blocks(tiles, 1), 256, 0, stream>>>(a, tiles, octs, parts);
+        else if constexpr (DT != 0) dropout_octets_kernel<DT><<<norm_blocks(tiles, 1), 256, 0, stream>>>(a, tiles, octs, parts);
     }
     return hipGetLastError();
 }

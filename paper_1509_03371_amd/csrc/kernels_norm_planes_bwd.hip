@@ -1,0 +1,250 @@
+// Layer norm of maps, backwards (see norm_tile.h).
+#include "norm_tile.h"
+
+namespace sk {
+
+namespace {
+
+// The gradients of an octet from its dy and s (both kept as they were read) and the four numbers of each pixel.
+// ADD: with dropout, dsum or dresidual.
+template <bool ADD, int DT, int LAYOUT, int P, int V>
+__device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, const NormBwdArgs &a, uint64_t counter, int o0,
+                                              typename Tile<DT, LAYOUT, P, V>::Octet &vy, typename Tile<DT, LAYOUT, P, V>::Octet &vs, const float (&gamma)[8],
+                                              const float (&mean)[V], const float (&rstd)[V], const float (&mg)[V], const float (&mgh)[V])
+{
+    const int left = t.channels(o0);
+    if (left <= 0 || !t.stores()) return;
+    const bool drops = ADD && a.drop.thresh && a.dx.p;
+    const uint32_t bits = drops ? t.mask(a.drop, counter, o0 + t.delta) : ~0u;
+    auto gradient = [&](int j, int v) {
+        const float h = (vs.at(j, v) - mean[v]) * rstd[v];
+        return rstd[v] * (vy.at(j, v) * gamma[j] - mg[v] - h * mgh[v]);
+    };
+    auto to_x = [&](int j, int v, float f) {
+        if (drops) f = kept(f, bits, 8 * v + j, a.drop);
+        return a.relu_x && !(vs.at(j, v) > 0.f) ? 0.f : f;
+    };
+    // a line at a time, each behind a branch of its own: together the values of all lines are more than the registers hold
+    auto lines = [&](const NormView &w) { return static_cast<dst_t>(w.p) + t.base(w, o0); };
+    const dst_t sum = ADD ? lines(a.dsum) : nullptr, residual = ADD ? lines(a.dresidual) : nullptr, x = lines(a.dx);
+    const uint32_t up_sum = ADD ? t.step(a.dsum) : 0, up_residual = ADD ? t.step(a.dresidual) : 0, up_x = t.step(a.dx);
+    constexpr bool maps = LAYOUT == MAPS;
+    constexpr int L = maps ? 8 : V, N = maps ? V : 8;   // lines, and elements of one
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        if (maps ? i >= left : !t.inside(i)) continue;
+        float f[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = maps ? gradient(i, e) : e < left ? gradient(e, i) : 0.f;
+        if (ADD && a.dsum.p) {
+            Words<DT, N> d;
+            d.load(sum, t.line(a.dsum, up_sum, i));
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[e] += d[e];
+        }
+        if (ADD && a.dresidual.p) store_at<DT, N>(residual, t.line(a.dresidual, up_residual, i), f);
+        if (ADD && !a.dx.p) continue;
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = maps ? to_x(i, e, f[e]) : to_x(e, i, f[e]);
+        store_at<DT, N>(x, t.line(a.dx, up_x, i), f);
+    }
+}
+
+// pixels of a thread: four 16-bit ones while a thread may have 256 registers (it takes 130 to 230), else two
+constexpr int bwd_pixels(int dtype, int threads) { return dtype == 0 || threads == 1024 ? 2 : 4; }
+
+// Backwards: a workgroup walks the tiles gridDim.x apart and keeps its threads' sums for dgamma and dbeta in registers until the end, where they go to the
+// workgroup's copy of the scratch, or to dgamma and dbeta themselves if there is one workgroup.
+template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(NormBwdArgs a, long tiles, long row)
+{
+    constexpr int V = bwd_pixels(DT, T);
+    extern __shared__ __align__(16) float part[];
+    Tile<DT, LAYOUT, P, V> t(a.plane, row, tiles, a.c);
+    const uint64_t counter = ADD ? a.drop.base() : 0;
+    const int c0 = 8 * t.octet(), left = a.c - c0;
+    float gamma[8], dg[8], db[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        gamma[j] = j >= left ? 0.f : a.gamma ? a.gamma[c0 + j] : 1.f;       // what does not count adds nothing to the sums over channels
+        dg[j] = db[j] = 0.f;
+    }
+    int half = 0;
+    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        t.go(tile);
+        typename Tile<DT, LAYOUT, P, V>::Octet vy, vs;
+        t.load(a.dy, t.oct0, vy);
+        t.load(a.s, t.oct0, vs);
+        float mean[V], rstd[V], sums[2][V] = {};
+        t.statistics(a.mean, mean);
+        t.statistics(a.rstd, rstd);
+        bool own[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) own[v] = t.own(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float h = (vs.at(j, v) - mean[v]) * rstd[v], y = vy.at(j, v), g = y * gamma[j], mine = own[v] ? y : 0.f;
+                sums[0][v] += g;
+                sums[1][v] += g * h;
+                dg[j] += mine * h;
+                db[j] += mine;
+            }
+        t.template total<2>(sums, part, half);
+        if (!a.dx.p && !a.dresidual.p) continue;
+        float mg[V], mgh[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            mg[v] = sums[0][v] / (float)a.c;
+            mgh[v] = sums[1][v] / (float)a.c;
+        }
+        vy.forget();
+        vs.forget();
+        put_gradients<ADD>(t, a, counter, t.oct0, vy, vs, gamma, mean, rstd, mg, mgh);
+    }
+    if (!a.dgamma && !a.dbeta) return;
+    // an octet belongs to the P lanes that hold its pixels
+    const bool alone = gridDim.x == 1;
+    const long cp = norm_copy_floats(a.c) / 2;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float *out = alone ? (which ? a.dbeta : a.dgamma) : a.scratch + (blockIdx.x * 2L + which) * cp;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float v = sum_lanes<P>(which ? db[j] : dg[j]);
+            if (out && t.lane == 0 && j < left) out[c0 + j] = v;
+        }
+    }
+}
+
+// As norm_deep_planes_kernel: read twice, and once more for the sums of dgamma and dbeta.
+template <int DT, int LAYOUT, int P, int V> __global__ __launch_bounds__(1024) void norm_deep_planes_bwd_kernel(NormBwdArgs a, long tiles, long row)
+{
+    extern __shared__ __align__(16) float part[];
+    Tile<DT, LAYOUT, P, V> t(a.plane, row, tiles, a.c);
+    const uint64_t counter = a.drop.base();
+    const int last = (a.c + 7) / 8, octs = blockDim.x / P;
+    int half = 0;
+    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        t.go(tile);
+        float mean[V], rstd[V], sums[2][V] = {}, mg[V], mgh[V], gamma[8];
+        t.statistics(a.mean, mean);
+        t.statistics(a.rstd, rstd);
+        typename Tile<DT, LAYOUT, P, V>::Octet vy, vs;
+        auto take = [&](int o0) {
+            t.load(a.dy, o0, vy);
+            t.load(a.s, o0, vs);
+            const int c0 = 8 * (o0 + t.delta);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) gamma[j] = c0 + j >= a.c ? 0.f : a.gamma ? a.gamma[c0 + j] : 1.f;
+        };
+        for (int o0 = t.oct0; o0 < last; o0 += octs) {
+            take(o0);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float q = 0.f, r = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float g = vy.at(j, v) * gamma[j];
+                    q += g;
+                    r += g * ((vs.at(j, v) - mean[v]) * rstd[v]);
+                }
+                sums[0][v] += q;
+                sums[1][v] += r;
+            }
+        }
+        t.template total<2>(sums, part, half);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            mg[v] = sums[0][v] / (float)a.c;
+            mgh[v] = sums[1][v] / (float)a.c;
+        }
+        for (int o0 = t.oct0; o0 < last; o0 += octs) {
+            take(o0);
+            put_gradients<true>(t, a, counter, o0, vy, vs, gamma, mean, rstd, mg, mgh);
+        }
+    }
+}
+
+// ... a wave an octet of channels, blockIdx.y a share of the tiles
+template <int DT, int LAYOUT, int V> __global__ __launch_bounds__(64) void norm_deep_planes_wgrad_kernel(NormBwdArgs a, long tiles, long row)
+{
+    Tile<DT, LAYOUT, 64, V> t(a.plane, row, tiles, a.c);
+    const long cp = norm_copy_floats(a.c) / 2;
+    for (int o = blockIdx.x; 8 * o < a.c; o += gridDim.x) {
+        float dg[8] = {}, db[8] = {};
+        for (long tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
+            t.go(tile);
+            typename Tile<DT, LAYOUT, 64, V>::Octet vy, vs;
+            float mean[V], rstd[V];
+            t.load(a.dy, o, vy);
+            t.load(a.s, o, vs);
+            t.statistics(a.mean, mean);
+            t.statistics(a.rstd, rstd);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float mine = t.own(v) ? vy.at(j, v) : 0.f;
+                    dg[j] += mine * ((vs.at(j, v) - mean[v]) * rstd[v]);
+                    db[j] += mine;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float g = sum_lanes<64>(dg[j]), s = sum_lanes<64>(db[j]);
+            if (t.lane == 0 && 8 * o + j < a.c) {
+                a.scratch[blockIdx.y * 2L * cp + 8 * o + j] = g;
+                a.scratch[(blockIdx.y * 2L + 1) * cp + 8 * o + j] = s;
+            }
+        }
+    }
+}
+
+}  // namespace
+
+// (a call whose strides 32 bits do not span takes fewer: it walks octets, whose copies are at most 16)
+int norm_planes_bwd_copies(const NormSpan &s)
+{
+    int copies = 16;
+    if (s.layout == OCTETS || s.plane >= 4)
+        pick_planes(s.c, [&](auto p, auto t, int threads) {
+            copies = (int)std::min<long>(s.n * tiles_of_image(s, p() * bwd_pixels(s.dtype, t())), 256 * std::max(1, 1024 / threads));
+        });
+    return copies;
+}
+
+hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t stream)
+{
+    auto fits = [&](int p) { return spans(a, p, {&a.dy, &a.s, &a.dsum, &a.dx, &a.dresidual}); };
+    const bool sums = a.dgamma || a.dbeta, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
+    pick_type(a, [&](auto dt, auto layout) {
+        bool done = false;
+        if (layout() == OCTETS || a.plane >= 4)
+            pick_planes(a.c, [&](auto p, auto t, int threads) {
+                if (!fits(p())) return;
+                const long row = tiles_of_image(a, p() * bwd_pixels(dt(), t())), tiles = a.n * row;
+                const size_t lds = part_bytes(2, p(), bwd_pixels(dt(), t()), threads);
+                if (adds) norm_planes_bwd_kernel<dt(), layout(), p(), t(), true><<<copies, threads, lds, stream>>>(a, tiles, row);
+                else norm_planes_bwd_kernel<dt(), layout(), p(), t(), false><<<copies, threads, lds, stream>>>(a, tiles, row);
+                if (sums && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
+                done = true;
+            });
+        if (done) return;
+        pick_deep(a, !fits(4), [&](auto p, auto v) {
+            if (sums) {
+                const long row = tiles_of_image(a, 64 * v()), tiles = a.n * row;
+                const int shares = (int)std::min<long>(std::min(copies, 16), tiles);
+                norm_deep_planes_wgrad_kernel<dt(), layout(), v()><<<dim3(std::min((a.c + 7) / 8, 65536), shares), 64, 0, stream>>>(a, tiles, row);
+                (void)launch_norm_reduce(a.scratch, shares, a.dgamma, a.dbeta, a.c, stream);
+            }
+            if (!a.dx.p && !a.dresidual.p) return;
+            const long row = tiles_of_image(a, p() * v()), tiles = a.n * row;
+            const int threads = deep_threads(a.c, p());
+            norm_deep_planes_bwd_kernel<dt(), layout(), p(), v()><<<norm_blocks(tiles, 1), threads, part_bytes(2, p(), v(), threads), stream>>>(a, tiles, row);
+        });
+    });
+    return hipGetLastError();
+}
+
+}  // namespace sk

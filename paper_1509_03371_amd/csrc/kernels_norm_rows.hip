@@ -8,6 +8,80 @@ namespace {
 
 // A row belongs to G lanes; lane l holds channels 8*(k*G + l) .. + 7 for k < K, the whole row in registers: one read of every input, one write of
 // every output, and the variance from the values themselves about their mean.  T threads a workgroup; G > 64: G = T, sums through LDS.
+template <int DT, int G> struct Row {
+    typedef elem_t<DT> E;
+    static constexpr int S = sizeof(E);
+    const int c;
+    const int lane, sub;                                // of the row's G; row among the wave's
+
+    __device__ __forceinline__ explicit Row(int c_) : c(c_), lane(threadIdx.x % G), sub(G < 64 ? (threadIdx.x & 63) / G : 0) {}
+    __device__ __forceinline__ int channel(int k) const { return 8 * (k * G + lane); }
+    // eight elements of a line of c, aligned to one of them.  A lane whose eight would reach over the line's end reads its last eight instead (lanes behind
+    // the end too): `fit` then puts them in place.
+    template <int D> __device__ __forceinline__ void load(src_t p, uint32_t off, int k, Words<D, 8> &w) const
+    {
+        constexpr int size = sizeof(elem_t<D>);
+        if constexpr (G == 1) {                         // lines of up to eight elements
+            w.clear();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < c) {
+                    if constexpr (D == 0) w.w[j] = *reinterpret_cast<const uint32_t *>(p + off + 4 * j);
+                    else w.w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p + off + 2 * j) << 16 * (j & 1);
+                }
+        } else {
+            w.load(p, off + size * std::min(channel(k), c - 8));
+        }
+    }
+    // zeros behind the line's end; `exact`: there is nothing behind it
+    template <int D> __device__ __forceinline__ void fit(int k, bool exact, Words<D, 8> &w) const
+    {
+        constexpr int n = Words<D, 8>::count;
+        if (G == 1 || exact) return;
+        const int left = c - channel(k);
+        if (c % 8) {                                    // down by 8 - c % 8 elements in the one lane that read over the end
+            const bool tail = left > 0 && left < 8;
+            const int down = 8 - c % 8;
+            auto words = [&](int by) {
+#pragma unroll
+                for (int i = 0; i < n; ++i) w.w[i] = tail ? (i + by < n ? w.w[i + by < n ? i + by : 0] : 0) : w.w[i];
+            };
+            if (down & 4) words(n / 2);
+            if (down & 2) words(n / 4);
+            if (down & 1) {
+                if constexpr (D == 0) {
+                    words(1);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < n; ++i) w.w[i] = tail ? (i + 1 < n ? __builtin_amdgcn_alignbit(w.w[i + 1 < n ? i + 1 : 0], w.w[i], 16) : w.w[i] >> 16) : w.w[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < n; ++i) w.w[i] = left > 0 ? w.w[i] : 0;
+    }
+    // row: the first of the wave's
+    __device__ __forceinline__ src_t from(const NormView &v, long row) const { return static_cast<src_t>(v.p) + S * row * v.sn; }
+    __device__ __forceinline__ uint32_t offset(const NormView &v) const { return G < 64 ? (uint32_t)sub * (uint32_t)(S * v.sn) : 0; }
+    __device__ __forceinline__ void store(const NormView &v, long row, int k, const float (&f)[8]) const
+    {
+        const int left = c - channel(k);
+        const dst_t p = static_cast<dst_t>(v.p) + S * row * v.sn;
+        const uint32_t off = offset(v) + S * channel(k);
+        if (left >= 8) {
+            store_at<DT, 8>(p, off, f);
+        } else if (left > 0) {                          // c % 8 elements, by four, two and one
+            const int r = c % 8;
+            auto one = [&](float a, float b, float c_, float d) { return (r & 4) ? ((r & 2) ? d : c_) : (r & 2) ? b : a; };       // (values, no places)
+            auto two = [&](float a, float b) { return (r & 4) ? b : a; };
+            if (r & 4) store_at<DT, 4>(p, off, {f[0], f[1], f[2], f[3]});
+            if (r & 2) store_at<DT, 2>(p, off + S * (r & 4), {two(f[0], f[4]), two(f[1], f[5])});
+            if (r & 1) store_at<DT, 1>(p, off + S * (r & 6), {one(f[0], f[2], f[4], f[6])});
+        }
+    }
+};
+
+// sum over a row's lanes, in every one of them
 template <int G> struct RowSum {
     float *part;                 // G > 64: two halves of G / 64 floats
     int half = 0;
@@ -27,83 +101,91 @@ template <int G> struct RowSum {
     }
 };
 
-template <int DT, int G, int K, int T> __global__ __launch_bounds__(T) void norm_rows_kernel(NormArgs a)
+// the first row of this wave; G > 64: of the workgroup
+template <int G, int T> __device__ __forceinline__ long first_row()
 {
-    typedef elem_t<DT> E;
+    if (G > 64) return blockIdx.x;
+    return (blockIdx.x * (long)(T / 64) + uniform(threadIdx.x >> 6)) * (64 / G);
+}
+template <int G, int T> __device__ __forceinline__ long row_step() { return G > 64 ? gridDim.x : gridDim.x * (long)(T / G); }
+
+// ADD: what is normalised is residual + dropout(x), or is wanted as an output
+template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T) void norm_rows_kernel(NormArgs a)
+{
     __shared__ float part[G > 64 ? 2 * (G / 64) : 1];
     RowSum<G> total{part};
-    const int lane = threadIdx.x % G;
-    const uint64_t base = a.drop.base();
-    for (long row = blockIdx.x * (long)(T / G) + threadIdx.x / G; row < a.n; row += gridDim.x * (long)(T / G)) {     // (G > 64: every thread alike)
-        const E *x = static_cast<const E *>(a.x.p) + row * a.x.sn;
+    const Row<DT, G> r(a.c);
+    const bool exact = a.c == 8 * G * K;
+    const uint64_t counter = ADD ? a.drop.base() : 0;
+    for (long row0 = first_row<G, T>(); row0 < a.n; row0 += row_step<G, T>()) {     // (G > 64: every thread alike)
+        const long row = row0 + r.sub;
+        if (G < 64 && row >= a.n) break;
         float s[K][8];
-        {
-            line_t<DT, 8> v[K];
+        Words<DT, 8> x[K], u[ADD ? K : 1];
 #pragma unroll
-            for (int k = 0; k < K; ++k) v[k] = load_line<DT, 8>(x, 8 * (k * G + lane), a.c);
+        for (int k = 0; k < K; ++k) r.load(r.from(a.x, row0), r.offset(a.x), k, x[k]);
+        if (ADD && a.residual.p)
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k) r.load(r.from(a.residual, row0), r.offset(a.residual), k, u[ADD ? k : 0]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s[k][j] = (float)v[k][j];
+        for (int k = 0; k < K; ++k) {
+            r.fit(k, exact, x[k]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[k][j] = x[k][j];
         }
-        if (a.drop.thresh) {
+        if (ADD && a.drop.thresh)
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 uint32_t w[4];
-                mask_words(w, a.drop, base, (uint64_t)row, k * G + lane);
+                mask_words(w, a.drop, counter, (uint64_t)row, k * G + r.lane);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[k][j] = dropped(s[k][j], w, j, a.drop);
             }
-        }
-        if (a.residual.p) {
-            const E *r = static_cast<const E *>(a.residual.p) + row * a.residual.sn;
-            line_t<DT, 8> v[K];
+        if (ADD && a.residual.p)
 #pragma unroll
-            for (int k = 0; k < K; ++k) v[k] = load_line<DT, 8>(r, 8 * (k * G + lane), a.c);
+            for (int k = 0; k < K; ++k) {
+                r.fit(k, exact, u[ADD ? k : 0]);
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[k][j] += (float)v[k][j];
-        }
+                for (int j = 0; j < 8; ++j) s[k][j] += u[ADD ? k : 0][j];
+            }
         float sum = 0.f, var = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += s[k][j];     // channels beyond the last are zeros
+            for (int j = 0; j < 8; ++j) sum += s[k][j];     // channels behind the last are zeros
         const float mean = total(sum) / (float)a.c;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = 8 * (k * G + lane) + j < a.c ? s[k][j] - mean : 0.f;
-                var += d * d;
+                const float d = s[k][j] - mean;
+                var += exact || r.channel(k) + j < a.c ? d * d : 0.f;
             }
         const float rstd = 1.f / sqrtf(total(var) / (float)a.c + a.eps);
-        E *y = static_cast<E *>(a.y.p) + row * a.y.sn;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c0 = 8 * (k * G + lane);
-            if (c0 >= a.c) break;
-            if (a.sum.p) store_line<DT, 8>(static_cast<E *>(a.sum.p) + row * a.sum.sn, c0, a.c, s[k]);
+            if (r.channel(k) >= a.c) continue;
+            if (ADD && a.sum.p) r.store(a.sum, row0, k, s[k]);
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = (s[k][j] - mean) * rstd;
             if (a.gamma) {
-                const line_t<0, 8> g = load_line<0, 8>(a.gamma, c0, a.c);
+                Words<0, 8> g;
+                r.load(reinterpret_cast<src_t>(a.gamma), 0, k, g);
+                r.fit(k, exact, g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[j] *= g[j];
             }
             if (a.beta) {
-                const line_t<0, 8> b = load_line<0, 8>(a.beta, c0, a.c);
+                Words<0, 8> b;
+                r.load(reinterpret_cast<src_t>(a.beta), 0, k, b);
+                r.fit(k, exact, b);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[j] += b[j];
             }
-            if (a.relu)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = o[j] < 0.f ? 0.f : o[j];
-            store_line<DT, 8>(y, c0, a.c, o);
+            r.store(a.y, row0, k, o);
         }
-        if (lane == 0) {
+        if (r.lane == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
@@ -113,61 +195,65 @@ template <int DT, int G, int K, int T> __global__ __launch_bounds__(T) void norm
 // Rows too long for the registers of a workgroup: read three times.
 template <int DT> __global__ __launch_bounds__(1024) void norm_long_rows_kernel(NormArgs a)
 {
-    typedef elem_t<DT> E;
     __shared__ float part[32];
     RowSum<1024> total{part};
+    const Row<DT, 1024> r(a.c);
+    const int K = (a.c + 8191) / 8192;
+    const uint64_t counter = a.drop.base();
     for (long row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const E *x = static_cast<const E *>(a.x.p) + row * a.x.sn, *r = static_cast<const E *>(a.residual.p) + row * a.residual.sn;
-        const uint64_t base = a.drop.base();
-        auto values = [&](int c0, float (&s)[8]) {
-            const line_t<DT, 8> v = load_line<DT, 8>(x, c0, a.c);
+        auto values = [&](int k, float (&s)[8]) {
+            Words<DT, 8> x, u;
+            r.load(r.from(a.x, row), 0, k, x);
+            if (a.residual.p) r.load(r.from(a.residual, row), 0, k, u);
+            r.fit(k, false, x);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] = (float)v[j];
+            for (int j = 0; j < 8; ++j) s[j] = x[j];
             if (a.drop.thresh) {
                 uint32_t w[4];
-                mask_words(w, a.drop, base, (uint64_t)row, (uint32_t)c0 >> 3);
+                mask_words(w, a.drop, counter, (uint64_t)row, k * 1024 + r.lane);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[j] = dropped(s[j], w, j, a.drop);
             }
             if (a.residual.p) {
-                const line_t<DT, 8> u = load_line<DT, 8>(r, c0, a.c);
+                r.fit(k, false, u);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] += (float)u[j];
+                for (int j = 0; j < 8; ++j) s[j] += u[j];
             }
         };
         float sum = 0.f, var = 0.f, s[8];
-        for (int c0 = 8 * threadIdx.x; c0 < a.c; c0 += 8192) {
-            values(c0, s);
+        for (int k = 0; k < K; ++k) {
+            values(k, s);
             float t = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) t += s[j];
             sum += t;
         }
         const float mean = total(sum) / (float)a.c;
-        for (int c0 = 8 * threadIdx.x; c0 < a.c; c0 += 8192) {
-            values(c0, s);
+        for (int k = 0; k < K; ++k) {
+            values(k, s);
             float t = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = c0 + j < a.c ? s[j] - mean : 0.f;
-                t += d * d;
+                const float d = s[j] - mean;
+                t += r.channel(k) + j < a.c ? d * d : 0.f;
             }
             var += t;
         }
         const float rstd = 1.f / sqrtf(total(var) / (float)a.c + a.eps);
-        for (int c0 = 8 * threadIdx.x; c0 < a.c; c0 += 8192) {
-            values(c0, s);
-            if (a.sum.p) store_line<DT, 8>(static_cast<E *>(a.sum.p) + row * a.sum.sn, c0, a.c, s);
+        for (int k = 0; k < K; ++k) {
+            values(k, s);
+            const int c0 = r.channel(k);
+            if (c0 >= a.c) break;
+            if (a.sum.p) r.store(a.sum, row, k, s);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float o = (s[j] - mean) * rstd;
+                s[j] = (s[j] - mean) * rstd;
                 if (c0 + j < a.c) {
-                    if (a.gamma) o *= a.gamma[c0 + j];
-                    if (a.beta) o += a.beta[c0 + j];
+                    if (a.gamma) s[j] *= a.gamma[c0 + j];
+                    if (a.beta) s[j] += a.beta[c0 + j];
                 }
-                s[j] = a.relu && o < 0.f ? 0.f : o;
             }
-            store_line<DT, 8>(static_cast<E *>(a.y.p) + row * a.y.sn, c0, a.c, s);
+            r.store(a.y, row, k, s);
         }
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -176,52 +262,86 @@ template <int DT> __global__ __launch_bounds__(1024) void norm_long_rows_kernel(
     }
 }
 
+// The gradient of a row's eight channels from its dy and s (kept as they were read) and the row's four numbers.  ADD: with dropout, dsum or dresidual.
+template <bool ADD, int DT, int G>
+__device__ __forceinline__ void put_gradients(const Row<DT, G> &r, const NormBwdArgs &a, uint64_t counter, long row0, int k, const Words<DT, 8> &vy,
+                                              const Words<DT, 8> &vs, const Words<DT, 8> &vd, const float (&gamma)[8], float mean, float rstd, float mg,
+                                              float mgh)
+{
+    float t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float h = (vs[j] - mean) * rstd;
+        t[j] = rstd * (vy[j] * gamma[j] - mg - h * mgh);
+    }
+    if (ADD) {
+        if (a.dsum.p)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] += vd[j];
+        if (a.dresidual.p) r.store(a.dresidual, row0, k, t);
+        if (!a.dx.p) return;
+        if (a.drop.thresh) {
+            uint32_t w[4];
+            mask_words(w, a.drop, counter, (uint64_t)(row0 + r.sub), k * G + r.lane);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = dropped(t[j], w, j, a.drop);
+        }
+    }
+    r.store(a.dx, row0, k, t);
+}
+
 // Backwards: a workgroup walks rows gridDim.x * T / G apart and keeps its lanes' sums for dgamma and dbeta in registers until the end, where they
 // go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta themselves if there is one workgroup.
-template <int DT, int G, int K, int T> __global__ __launch_bounds__(T) void norm_rows_bwd_kernel(NormBwdArgs a)
+template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T) void norm_rows_bwd_kernel(NormBwdArgs a)
 {
-    typedef elem_t<DT> E;
-    constexpr int R = T / G;                            // rows at a time
     constexpr int W = T / 64;
     __shared__ float part[G > 64 ? 4 * W : 1];
-    __shared__ float sums[G < T ? W : 1][G < T ? 64 * K * 8 + 1 : 1];
-    const int lane = threadIdx.x % G;
-    const uint64_t base = a.drop.base();
+    __shared__ float sums[G < T ? W : 1][G < T ? G * K * 8 + 1 : 1];
+    const Row<DT, G> r(a.c);
+    const bool exact = a.c == 8 * G * K;
+    const uint64_t counter = ADD ? a.drop.base() : 0;
     float gamma[K][8], dg[K][8], db[K][8];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int c0 = 8 * (k * G + lane);
-        const line_t<0, 8> g = a.gamma ? load_line<0, 8>(a.gamma, c0, a.c) : line_t<0, 8>{};
+        Words<0, 8> g;
+        if (a.gamma) {
+            r.load(reinterpret_cast<src_t>(a.gamma), 0, k, g);
+            r.fit(k, exact, g);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            gamma[k][j] = a.gamma ? g[j] : c0 + j < a.c ? 1.f : 0.f;
+            gamma[k][j] = a.gamma ? g[j] : 1.f;
             dg[k][j] = db[k][j] = 0.f;
         }
     }
     int half = 0;
-    for (long row = blockIdx.x * (long)R + threadIdx.x / G; row < a.n; row += gridDim.x * (long)R) {     // (G > 64: R = 1, every thread alike)
-        const E *dy = static_cast<const E *>(a.dy.p) + row * a.dy.sn, *s = static_cast<const E *>(a.s.p) + row * a.s.sn;
-        line_t<DT, 8> vy[K], vs[K], vd[K];
+    for (long row0 = first_row<G, T>(); row0 < a.n; row0 += row_step<G, T>()) {     // (G > 64: every thread alike)
+        const long row = row0 + r.sub;
+        if (G < 64 && row >= a.n) break;
+        Words<DT, 8> vy[K], vs[K], vd[ADD ? K : 1];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            vy[k] = load_line<DT, 8>(dy, 8 * (k * G + lane), a.c);
-            vs[k] = load_line<DT, 8>(s, 8 * (k * G + lane), a.c);
+            r.load(r.from(a.dy, row0), r.offset(a.dy), k, vy[k]);
+            r.load(r.from(a.s, row0), r.offset(a.s), k, vs[k]);
         }
-        if (a.dsum.p)
+        if (ADD && a.dsum.p)
 #pragma unroll
-            for (int k = 0; k < K; ++k) vd[k] = load_line<DT, 8>(static_cast<const E *>(a.dsum.p) + row * a.dsum.sn, 8 * (k * G + lane), a.c);
+            for (int k = 0; k < K; ++k) r.load(r.from(a.dsum, row0), r.offset(a.dsum), k, vd[ADD ? k : 0]);
         const float mean = a.mean[row], rstd = a.rstd[row];
         float sg = 0.f, sgh = 0.f;
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) {
+            r.fit(k, exact, vy[k]);                     // behind the last channel dy is zero
+            r.fit(k, exact, vs[k]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float h = ((float)vs[k][j] - mean) * rstd, y = (float)vy[k][j], g = y * gamma[k][j];     // beyond the last channel y is zero
+                const float h = (vs[k][j] - mean) * rstd, y = vy[k][j], g = y * gamma[k][j];
                 sg += g;
                 sgh += g * h;
                 dg[k][j] += y * h;
                 db[k][j] += y;
             }
+        }
         sg = sum_lanes<(G < 64 ? G : 64)>(sg);
         sgh = sum_lanes<(G < 64 ? G : 64)>(sgh);
         if (G > 64) {
@@ -239,51 +359,29 @@ template <int DT, int G, int K, int T> __global__ __launch_bounds__(T) void norm
                 sgh += p[W + i];
             }
         }
-        if (!a.dx.p && !a.dresidual.p) continue;
+        if (!a.dx.p && (!ADD || !a.dresidual.p)) continue;
         const float mg = sg / (float)a.c, mgh = sgh / (float)a.c;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c0 = 8 * (k * G + lane);
-            if (c0 >= a.c) break;
-            float t[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float h = ((float)vs[k][j] - mean) * rstd;
-                t[j] = rstd * ((float)vy[k][j] * gamma[k][j] - mg - h * mgh);
-            }
-            if (a.dsum.p)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] += (float)vd[k][j];
-            if (a.dresidual.p) store_line<DT, 8>(static_cast<E *>(a.dresidual.p) + row * a.dresidual.sn, c0, a.c, t);
-            if (!a.dx.p) continue;
-            if (a.drop.thresh) {
-                uint32_t w[4];
-                mask_words(w, a.drop, base, (uint64_t)row, k * G + lane);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = dropped(t[j], w, j, a.drop);
-            }
-            if (a.relu_x)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = (float)vs[k][j] > 0.f ? t[j] : 0.f;
-            store_line<DT, 8>(static_cast<E *>(a.dx.p) + row * a.dx.sn, c0, a.c, t);
+            if (r.channel(k) >= a.c) continue;
+            vy[k].forget();
+            vs[k].forget();
+            if (ADD && a.dsum.p) r.fit(k, exact, vd[ADD ? k : 0]);
+            put_gradients<ADD>(r, a, counter, row0, k, vy[k], vs[k], vd[ADD ? k : 0], gamma[k], mean, rstd, mg, mgh);
         }
     }
     if (!a.dgamma && !a.dbeta) return;
     const bool alone = gridDim.x == 1;
     const long cp = norm_copy_floats(a.c) / 2;
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        float(&acc)[K][8] = which ? db : dg;
-        float *out = alone ? (which ? a.dbeta : a.dgamma) : a.scratch + (blockIdx.x * 2L + which) * cp;
-        const long count = alone ? a.c : cp;            // a copy's tail holds zeros
+    auto put = [&](const float (&acc)[K][8], float *own, int which) {
+        float *out = alone ? own : a.scratch + (blockIdx.x * 2L + which) * cp;
         if (G == T) {                                   // every channel belongs to one lane of the workgroup
+            const Row<0, G> f(a.c);
+            const NormView v{out, 0, 0};
             if (out)
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const int c0 = 8 * (k * G + lane);
-                    if (c0 < count) store_line<0, 8>(out, c0, count, acc[k]);
-                }
-            continue;
+                for (int k = 0; k < K; ++k) f.store(v, 0, k, acc[k]);
+            return;
         }
         // rows of one wave first, then the waves in order
 #pragma unroll
@@ -293,146 +391,138 @@ template <int DT, int G, int K, int T> __global__ __launch_bounds__(T) void norm
                 float v = acc[k][j];
 #pragma unroll
                 for (int i = G; i < 64; i *= 2) v += __shfl_xor(v, i);
-                if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][8 * (k * G + lane) + j] = v;
+                if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][8 * (k * G + r.lane) + j] = v;
             }
         __syncthreads();
         if (out)
-            for (int c = threadIdx.x; c < count; c += T) {
+            for (int c = threadIdx.x; c < a.c; c += T) {
                 float v = 0.f;
-                if (c < 8 * K * G)
 #pragma unroll
-                    for (int i = 0; i < W; ++i) v += sums[i][c];
+                for (int i = 0; i < W; ++i) v += sums[i][c];
                 out[c] = v;
             }
         __syncthreads();
-    }
+    };
+    put(dg, a.dgamma, 0);
+    put(db, a.dbeta, 1);
 }
 
 // Rows too long for the registers: read twice; the sums of dgamma and dbeta by a walk over the rows per channel.
 template <int DT> __global__ __launch_bounds__(1024) void norm_long_rows_bwd_kernel(NormBwdArgs a)
 {
-    typedef elem_t<DT> E;
     __shared__ float part[32];
     RowSum<1024> total{part};
+    const Row<DT, 1024> r(a.c);
+    const int K = (a.c + 8191) / 8192;
+    const uint64_t counter = a.drop.base();
     for (long row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const E *dy = static_cast<const E *>(a.dy.p) + row * a.dy.sn, *s = static_cast<const E *>(a.s.p) + row * a.s.sn;
-        const uint64_t base = a.drop.base();
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float sg = 0.f, sgh = 0.f;
-        auto both = [&](int c0, float (&g)[8], float (&v)[8]) {
-            const line_t<DT, 8> vy = load_line<DT, 8>(dy, c0, a.c), vs = load_line<DT, 8>(s, c0, a.c);
+        float sg = 0.f, sgh = 0.f, gamma[8];
+        Words<DT, 8> vy, vs, vd;
+        auto both = [&](int k) {
+            r.load(r.from(a.dy, row), 0, k, vy);
+            r.load(r.from(a.s, row), 0, k, vs);
+            r.fit(k, false, vy);
+            r.fit(k, false, vs);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = (float)vs[j];
-                g[j] = (float)vy[j] * (a.gamma && c0 + j < a.c ? a.gamma[c0 + j] : 1.f);
-            }
+            for (int j = 0; j < 8; ++j) gamma[j] = a.gamma && r.channel(k) + j < a.c ? a.gamma[r.channel(k) + j] : 1.f;
         };
-        float g[8], v[8];
-        for (int c0 = 8 * threadIdx.x; c0 < a.c; c0 += 8192) {
-            both(c0, g, v);
+        for (int k = 0; k < K; ++k) {
+            both(k);
             float t0 = 0.f, t1 = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                t0 += g[j];
-                t1 += g[j] * ((v[j] - mean) * rstd);
+                t0 += vy[j] * gamma[j];
+                t1 += vy[j] * gamma[j] * ((vs[j] - mean) * rstd);
             }
             sg += t0;
             sgh += t1;
         }
         const float mg = total(sg) / (float)a.c, mgh = total(sgh) / (float)a.c;
-        for (int c0 = 8 * threadIdx.x; c0 < a.c; c0 += 8192) {
-            both(c0, g, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = rstd * (g[j] - mg - (v[j] - mean) * rstd * mgh);
+        for (int k = 0; k < K; ++k) {
+            both(k);
             if (a.dsum.p) {
-                const line_t<DT, 8> d = load_line<DT, 8>(static_cast<const E *>(a.dsum.p) + row * a.dsum.sn, c0, a.c);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] += (float)d[j];
+                r.load(r.from(a.dsum, row), 0, k, vd);
+                r.fit(k, false, vd);
             }
-            if (a.dresidual.p) store_line<DT, 8>(static_cast<E *>(a.dresidual.p) + row * a.dresidual.sn, c0, a.c, g);
-            if (!a.dx.p) continue;
-            if (a.drop.thresh) {
-                uint32_t w[4];
-                mask_words(w, a.drop, base, (uint64_t)row, (uint32_t)c0 >> 3);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = dropped(g[j], w, j, a.drop);
-            }
-            if (a.relu_x)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = v[j] > 0.f ? g[j] : 0.f;
-            store_line<DT, 8>(static_cast<E *>(a.dx.p) + row * a.dx.sn, c0, a.c, g);
+            if (r.channel(k) < a.c) put_gradients<true>(r, a, counter, row, k, vy, vs, vd, gamma, mean, rstd, mg, mgh);
         }
     }
 }
 
 // dgamma and dbeta of rows too long for registers: a thread eight channels, blockIdx.y a share of the rows
-template <int DT> __global__ __launch_bounds__(256) void norm_long_rows_wgrad_kernel(NormBwdArgs a)
+template <int DT> __global__ __launch_bounds__(1024) void norm_long_rows_wgrad_kernel(NormBwdArgs a)
 {
-    typedef elem_t<DT> E;
-    const int c0 = 8 * (blockIdx.x * 256 + threadIdx.x);
+    const Row<DT, 1024> r(a.c);
     const long cp = norm_copy_floats(a.c) / 2;
-    if (c0 >= cp) return;
-    float dg[8] = {}, db[8] = {};
-    for (long row = blockIdx.y; row < a.n; row += gridDim.y) {
-        const line_t<DT, 8> vy = load_line<DT, 8>(static_cast<const E *>(a.dy.p) + row * a.dy.sn, c0, a.c);
-        const line_t<DT, 8> vs = load_line<DT, 8>(static_cast<const E *>(a.s.p) + row * a.s.sn, c0, a.c);
-        const float mean = a.mean[row], rstd = a.rstd[row];
+    for (int k = blockIdx.x; k < (a.c + 8191) / 8192; k += gridDim.x) {
+        float dg[8] = {}, db[8] = {};
+        for (long row = blockIdx.y; row < a.n; row += gridDim.y) {
+            Words<DT, 8> vy, vs;
+            r.load(r.from(a.dy, row), 0, k, vy);
+            r.load(r.from(a.s, row), 0, k, vs);
+            const float mean = a.mean[row], rstd = a.rstd[row];
+            r.fit(k, false, vy);
+            r.fit(k, false, vs);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            dg[j] += (float)vy[j] * (((float)vs[j] - mean) * rstd);
-            db[j] += (float)vy[j];
+            for (int j = 0; j < 8; ++j) {
+                dg[j] += vy[j] * ((vs[j] - mean) * rstd);
+                db[j] += vy[j];
+            }
         }
+        const Row<0, 1024> f(a.c);
+        f.store(NormView{a.scratch + blockIdx.y * 2L * cp, 0, 0}, 0, k, dg);
+        f.store(NormView{a.scratch + (blockIdx.y * 2L + 1) * cp, 0, 0}, 0, k, db);
     }
-    float *out = a.scratch + blockIdx.y * 2L * cp;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (c0 + j < cp) {
-            out[c0 + j] = c0 + j < a.c ? dg[j] : 0.f;
-            out[cp + c0 + j] = c0 + j < a.c ? db[j] : 0.f;
-        }
 }
 
-constexpr int kLongRow = 32768;                         // from here on rows do not fit the registers of a workgroup
+constexpr int kLongRow = 32768, kLongRowBwd = 16384;    // longer rows do not fit the registers of a workgroup
 
-// f(G, K, T) for rows of c channels, forwards
-template <class F> hipError_t pick_rows(int c, F f)
+template <int N> using num = std::integral_constant<int, N>;
+
+// f(G, K, T) for rows of c channels, forwards; far: rows so far apart that 32 bits do not span those of a wave
+template <class F> void pick_rows(int c, bool far, F f)
 {
-#define SK_ROWS_CASE(most, G, K, T) if (c <= most) return f(std::integral_constant<int, G>{}, std::integral_constant<int, K>{}, std::integral_constant<int, T>{})
-    SK_ROWS_CASE(8, 1, 1, 256);
-    SK_ROWS_CASE(64, 8, 1, 256);
-    SK_ROWS_CASE(128, 16, 1, 256);
-    SK_ROWS_CASE(256, 32, 1, 256);
-    SK_ROWS_CASE(512, 64, 1, 256);
-    SK_ROWS_CASE(1024, 64, 2, 256);
-    SK_ROWS_CASE(2048, 64, 4, 256);
-    SK_ROWS_CASE(4096, 256, 2, 256);
-    SK_ROWS_CASE(8192, 256, 4, 256);
-    SK_ROWS_CASE(16384, 1024, 2, 1024);
-    return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 1024>{});
+    if (c <= 8 && !far) return f(num<1>{}, num<1>{}, num<256>{});
+    if (c <= 64 && !far) return f(num<8>{}, num<1>{}, num<256>{});
+    if (c <= 128 && !far) return f(num<16>{}, num<1>{}, num<256>{});
+    if (c <= 256 && !far) return f(num<32>{}, num<1>{}, num<256>{});
+    if (c <= 512) return f(num<64>{}, num<1>{}, num<256>{});
+    if (c <= 1024) return f(num<64>{}, num<2>{}, num<256>{});
+    if (c <= 2048) return f(num<64>{}, num<4>{}, num<256>{});
+    if (c <= 4096) return f(num<256>{}, num<2>{}, num<256>{});
+    if (c <= 8192) return f(num<256>{}, num<4>{}, num<256>{});
+    if (c <= 16384) return f(num<1024>{}, num<2>{}, num<1024>{});
+    return f(num<1024>{}, num<4>{}, num<1024>{});
 }
 
 // the same backwards, where a lane also holds gamma and two sums a channel
-template <class F> hipError_t pick_rows_bwd(int c, F f)
+template <class F> void pick_rows_bwd(int c, bool far, F f)
 {
-    SK_ROWS_CASE(8, 1, 1, 256);
-    SK_ROWS_CASE(64, 8, 1, 256);
-    SK_ROWS_CASE(128, 16, 1, 256);
-    SK_ROWS_CASE(256, 32, 1, 256);
-    SK_ROWS_CASE(512, 64, 1, 256);
-    SK_ROWS_CASE(1024, 64, 2, 256);
-    SK_ROWS_CASE(2048, 128, 2, 128);
-    SK_ROWS_CASE(4096, 256, 2, 256);
-    SK_ROWS_CASE(8192, 512, 2, 512);
-    SK_ROWS_CASE(16384, 1024, 2, 1024);
-    return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 1024>{});
-#undef SK_ROWS_CASE
+    if (c <= 8 && !far) return f(num<1>{}, num<1>{}, num<256>{});
+    if (c <= 64 && !far) return f(num<8>{}, num<1>{}, num<256>{});
+    if (c <= 128 && !far) return f(num<16>{}, num<1>{}, num<256>{});
+    if (c <= 256 && !far) return f(num<32>{}, num<1>{}, num<256>{});
+    if (c <= 512) return f(num<64>{}, num<1>{}, num<256>{});
+    if (c <= 1024) return f(num<64>{}, num<2>{}, num<256>{});
+    if (c <= 2048) return f(num<128>{}, num<2>{}, num<128>{});
+    if (c <= 4096) return f(num<256>{}, num<2>{}, num<256>{});
+    if (c <= 8192) return f(num<512>{}, num<2>{}, num<512>{});
+    return f(num<1024>{}, num<2>{}, num<1024>{});
 }
 
-template <class F> hipError_t pick_type(int dtype, F f)
+bool far_apart(std::initializer_list<const NormView *> views)
 {
-    if (dtype == 0) return f(std::integral_constant<int, 0>{});
-    if (dtype == 1) return f(std::integral_constant<int, 1>{});
-    return f(std::integral_constant<int, 2>{});
+    for (const NormView *v : views)
+        if (v->p && v->sn >= (1L << 24)) return true;   // 64 rows of elements of at most four bytes
+    return false;
+}
+
+template <class F> void pick_type(int dtype, F f)
+{
+    if (dtype == 0) return f(num<0>{});
+    if (dtype == 1) return f(num<1>{});
+    return f(num<2>{});
 }
 
 __global__ __launch_bounds__(256) void norm_reduce_kernel(const float *scratch, int copies, float *dgamma, float *dbeta, int c)
@@ -456,46 +546,51 @@ hipError_t launch_norm_reduce(const float *scratch, int copies, float *dgamma, f
 
 hipError_t launch_norm_rows(const NormArgs &a, hipStream_t stream)
 {
-    return pick_type(a.dtype, [&](auto dt) {
+    if (a.relu) return hipErrorInvalidValue;            // (a net's layers are maps)
+    const bool adds = a.residual.p || a.sum.p || a.drop.thresh, far = far_apart({&a.x, &a.residual, &a.sum, &a.y});
+    pick_type(a.dtype, [&](auto dt) {
         if (a.c > kLongRow) {
             norm_long_rows_kernel<dt()><<<norm_blocks(a.n, 1), 1024, 0, stream>>>(a);
-            return hipGetLastError();
+            return;
         }
-        return pick_rows(a.c, [&](auto g, auto k, auto t) {
-            norm_rows_kernel<dt(), g(), k(), t()><<<norm_blocks(a.n, t() / g()), t(), 0, stream>>>(a);
-            return hipGetLastError();
+        pick_rows(a.c, far, [&](auto g, auto k, auto t) {
+            if (adds) norm_rows_kernel<dt(), g(), k(), t(), true><<<norm_blocks(a.n, t() / g()), t(), 0, stream>>>(a);
+            else norm_rows_kernel<dt(), g(), k(), t(), false><<<norm_blocks(a.n, t() / g()), t(), 0, stream>>>(a);
         });
     });
+    return hipGetLastError();
 }
 
+// (rows far apart take as many: their workgroups hold no more of them)
 int norm_rows_bwd_copies(const NormSpan &s)
 {
-    if (s.c > kLongRow) return (int)std::min<long>(s.n, 16);
+    if (s.c > kLongRowBwd) return (int)std::min<long>(s.n, 16);
     int copies = 1;
-    (void)pick_rows_bwd(s.c, [&](auto g, auto, auto t) {
-        copies = (int)std::min<long>((s.n + t() / g() - 1) / (t() / g()), 256 * 1024 / t());
-        return hipSuccess;
-    });
+    pick_rows_bwd(s.c, false, [&](auto g, auto, auto t) { copies = (int)std::min<long>((s.n + t() / g() - 1) / (t() / g()), 256 * 1024 / t()); });
     return copies;
 }
 
 hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t stream)
 {
-    return pick_type(a.dtype, [&](auto dt) {
-        if (a.c > kLongRow) {
-            if (a.dgamma || a.dbeta) {
-                norm_long_rows_wgrad_kernel<dt()><<<dim3((unsigned)((a.c + 2047) / 2048), copies), 256, 0, stream>>>(a);
-                if (hipError_t e = launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream)) return e;
+    if (a.relu_x) return hipErrorInvalidValue;
+    const bool sums = a.dgamma || a.dbeta, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
+    const bool far = far_apart({&a.dy, &a.s, &a.dsum, &a.dx, &a.dresidual});
+    pick_type(a.dtype, [&](auto dt) {
+        if (a.c > kLongRowBwd) {
+            if (sums) {
+                norm_long_rows_wgrad_kernel<dt()><<<dim3((unsigned)std::min((a.c + 8191) / 8192, 65536), std::min(copies, 16)), 1024, 0, stream>>>(a);
+                (void)launch_norm_reduce(a.scratch, std::min(copies, 16), a.dgamma, a.dbeta, a.c, stream);
             }
             if (a.dx.p || a.dresidual.p) norm_long_rows_bwd_kernel<dt()><<<norm_blocks(a.n, 1), 1024, 0, stream>>>(a);
-            return hipGetLastError();
+            return;
         }
-        return pick_rows_bwd(a.c, [&](auto g, auto k, auto t) {
-            norm_rows_bwd_kernel<dt(), g(), k(), t()><<<copies, t(), 0, stream>>>(a);
-            if ((a.dgamma || a.dbeta) && copies > 1) return launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
-            return hipGetLastError();
+        pick_rows_bwd(a.c, far, [&](auto g, auto k, auto t) {
+            if (adds) norm_rows_bwd_kernel<dt(), g(), k(), t(), true><<<copies, t(), 0, stream>>>(a);
+            else norm_rows_bwd_kernel<dt(), g(), k(), t(), false><<<copies, t(), 0, stream>>>(a);
+            if (sums && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
         });
     });
+    return hipGetLastError();
 }
 
 }  // namespace sk

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "norm.h"
@@ -22,29 +23,59 @@ template <int DT, int N> struct Line {
 };
 template <int DT, int N> using line_t = typename Line<DT, N>::type;
 
-// elements first .. first + N - 1 of a line of `count`; zeros where it has none
-template <int DT, int N> __device__ __forceinline__ line_t<DT, N> load_line(const elem_t<DT> *p, long first, long count)
+// Addresses are a base that is equal in all lanes of a wave and 32 bits a lane: one register a lane instead of two, and the additions on the
+// scalar unit.  `off` counts bytes.
+typedef const char *src_t;
+typedef char *dst_t;
+template <int DT, int N> __device__ __forceinline__ line_t<DT, N> load_at(src_t base, uint32_t off)
+{
+    return *reinterpret_cast<const line_t<DT, N> *>(base + off);
+}
+template <int DT, int N> __device__ __forceinline__ void store_at(dst_t base, uint32_t off, const float (&f)[N])
 {
     line_t<DT, N> v;
-    if (first + N <= count) return *reinterpret_cast<const line_t<DT, N> *>(p + first);
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = first + j < count ? p[first + j] : static_cast<elem_t<DT>>(0.f);
-    return v;
+    for (int j = 0; j < N; ++j) v[j] = static_cast<elem_t<DT>>(f[j]);
+    *reinterpret_cast<line_t<DT, N> *>(base + off) = v;
 }
 
-template <int DT, int N> __device__ __forceinline__ void store_line(elem_t<DT> *p, long first, long count, const float (&f)[N])
-{
-    if (first + N <= count) {
-        line_t<DT, N> v;
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// N elements as the words that hold them, which is how they stay in registers: 16-bit ones are widened at each use
+template <int DT, int N> struct Words {
+    static constexpr int count = (N * (DT == 0 ? 4 : 2) + 3) / 4;
+    uint32_t w[count];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = static_cast<elem_t<DT>>(f[j]);
-        *reinterpret_cast<line_t<DT, N> *>(p + first) = v;
-        return;
+        for (int i = 0; i < count; ++i) w[i] = 0;
     }
+    __device__ __forceinline__ void load(src_t base, uint32_t off)
+    {
+        if constexpr (N == 1) {
+            if constexpr (DT == 0) w[0] = __float_as_uint(*reinterpret_cast<const float *>(base + off));
+            else w[0] = *reinterpret_cast<const uint16_t *>(base + off);
+        } else {
+            typedef uint32_t Line __attribute__((ext_vector_type(count), aligned(sizeof(elem_t<DT>))));
+            const Line v = *reinterpret_cast<const Line *>(base + off);
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-        if (first + j < count) p[first + j] = static_cast<elem_t<DT>>(f[j]);
-}
+            for (int i = 0; i < count; ++i) w[i] = v[i];
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (DT == 0) return __uint_as_float(w[i]);
+        else if constexpr (DT == 1) return __uint_as_float((i & 1) ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)((i & 1) ? w[i / 2] >> 16 : w[i / 2]));
+    }
+    // the next use is to widen again, not to find the fp32 value still in a register
+    __device__ __forceinline__ void forget()
+    {
+        if constexpr (DT != 0)
+#pragma unroll
+            for (int i = 0; i < count; ++i) asm volatile("" : "+v"(w[i]));
+    }
+};
 
 // v + the v of the lane whose number differs in bit STEP, over lanes whose lower bits are summed already (STEP 4 and 8: mirrored
 // halves, of which every lane of a half holds the same); exchanges within sixteen lanes are operand modifiers, not LDS traffic

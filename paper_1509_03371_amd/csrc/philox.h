@@ -50,4 +50,23 @@ __device__ __forceinline__ float dropped(float v, const uint32_t (&w)[4], int j,
     return u >= m.thresh ? v * m.scale : 0.f;
 }
 
+// the mask of an octet as bits, channel j at bit FIRST + j (dropped: 0): one register for four positions
+template <int FIRST> __device__ __forceinline__ uint32_t keep_bits(const uint32_t (&w)[4], const DropMask &m)
+{
+    uint32_t bits = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t u = (j & 1) ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu;
+        bits |= (u >= m.thresh ? 1u : 0u) << (FIRST + j);
+    }
+    return bits;
+}
+
+// v scaled where the bit is set, else zero (of NaN and infinity too)
+__device__ __forceinline__ float kept(float v, uint32_t bits, int bit, const DropMask &m)
+{
+    const int all = (int)(bits << (31 - bit)) >> 31;     // 0 or -1
+    return __uint_as_float(__float_as_uint(v * m.scale) & (uint32_t)all);
+}
+
 }  // namespace sk
