@@ -34,18 +34,20 @@ template <int DT> __global__ __launch_bounds__(256) void dropout_rows_kernel(Dro
     }
 }
 
-// Maps: a thread takes an octet of channels of V pixels side by side.  Lanes whose pixels would reach over the plane's end take its last V instead (those
-// that two lanes of a wave then hold are computed alike and stored twice, after both have read).
+// Maps: a thread takes an octet of channels of V pixels side by side, a wave a stretch of 64 V.
 template <int DT, int V> __global__ __launch_bounds__(256) void dropout_maps_kernel(DropoutArgs a, long tiles, int octs, long parts)
 {
     typedef elem_t<DT> E;
     const uint64_t counter = a.drop.base();
+    const uint32_t mine = V * (threadIdx.x & 63);
     for (long t = blockIdx.x; t < tiles; t += gridDim.x) {          // tile: (image, octet, part of the plane), the last fastest
-        const long line = t / parts, b = line / octs, first = t % parts * 256L * V, begin = first + threadIdx.x * V;
+        const long line = t / parts, b = line / octs, first = (t % parts * 4 + uniform(threadIdx.x >> 6)) * (64L * V);
         const int o = (int)(line % octs), left = a.c - 8 * o;
-        if (begin >= a.plane) continue;
-        const long from = first < a.plane - V ? first : a.plane - V;
-        const uint32_t px = (uint32_t)((begin < a.plane - V ? begin : a.plane - V) - from), off = px * sizeof(E);
+        if (first >= a.plane) continue;
+        const Stretch<V> run(first, 64 * V, a.plane, mine);
+        if (run.empty(mine)) continue;
+        const long from = run.start;
+        const uint32_t px = run.at, off = px * sizeof(E);
         src_t x = reinterpret_cast<src_t>(static_cast<const E *>(a.x.p) + b * a.x.sn + 8L * o * a.x.sc + from);
         dst_t y = reinterpret_cast<dst_t>(static_cast<E *>(a.y.p) + b * a.y.sn + 8L * o * a.y.sc + from);
         const long up_x = a.x.sc * sizeof(E), up_y = a.y.sc * sizeof(E), up_r = a.relu_src.sc * sizeof(E);

@@ -14,7 +14,7 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
     Tile<DT, LAYOUT, P, V> t(a.plane, row, tiles, a.c);
     const uint64_t counter = ADD ? a.drop.base() : 0;
     int half = 0;
-    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (long tile = neighbour(); tile < tiles; tile += gridDim.x) {
         t.go(tile);
         float s[8][V], sum[1][V] = {}, var[1][V] = {}, mean[V], rstd[V];
         t.template values<ADD>(a, counter, t.oct0, s);
@@ -40,7 +40,7 @@ template <int DT, int LAYOUT, int P, int V> __global__ __launch_bounds__(1024) v
     const uint64_t counter = a.drop.base();
     const int last = (a.c + 7) / 8, octs = blockDim.x / P;
     int half = 0;
-    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (long tile = neighbour(); tile < tiles; tile += gridDim.x) {
         t.go(tile);
         float s[8][V], sum[1][V] = {}, var[1][V] = {}, mean[V], rstd[V];
         for (int o0 = t.oct0; o0 < last; o0 += octs) {
@@ -74,7 +74,7 @@ hipError_t launch_norm_planes(const NormArgs &a, hipStream_t stream)
     pick_type(a, [&](auto dt, auto layout) {
         bool done = false;
         if (layout() == OCTETS || a.plane >= 4)
-            pick_planes(a.c, [&](auto p, auto t, int threads) {
+            pick_planes<false>(a.c, [&](auto p, auto t, int threads) {
                 if (!fits(p())) return;
                 const long row = tiles_of_image(a, p() * 4), tiles = a.n * row;
                 const size_t lds = part_bytes(1, p(), 4, threads);

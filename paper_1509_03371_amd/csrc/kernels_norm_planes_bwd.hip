@@ -28,6 +28,7 @@ __device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, c
     auto lines = [&](const NormView &w) { return static_cast<dst_t>(w.p) + t.base(w, o0); };
     const dst_t sum = ADD ? lines(a.dsum) : nullptr, residual = ADD ? lines(a.dresidual) : nullptr, x = lines(a.dx);
     const uint32_t up_sum = ADD ? t.step(a.dsum) : 0, up_residual = ADD ? t.step(a.dresidual) : 0, up_x = t.step(a.dx);
+    const uint32_t off_sum = t.first(up_sum), off_residual = t.first(up_residual), off_x = t.first(up_x);
     constexpr bool maps = LAYOUT == MAPS;
     constexpr int L = maps ? 8 : V, N = maps ? V : 8;   // lines, and elements of one
 #pragma unroll
@@ -38,38 +39,39 @@ __device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, c
         for (int e = 0; e < N; ++e) f[e] = maps ? gradient(i, e) : e < left ? gradient(e, i) : 0.f;
         if (ADD && a.dsum.p) {
             Words<DT, N> d;
-            d.load(sum, t.line(a.dsum, up_sum, i));
+            d.load(sum, off_sum + i * t.next(up_sum));
 #pragma unroll
             for (int e = 0; e < N; ++e) f[e] += d[e];
         }
-        if (ADD && a.dresidual.p) store_at<DT, N>(residual, t.line(a.dresidual, up_residual, i), f);
+        if (ADD && a.dresidual.p) store_at<DT, N>(residual, off_residual + i * t.next(up_residual), f);
         if (ADD && !a.dx.p) continue;
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] = maps ? to_x(i, e, f[e]) : to_x(e, i, f[e]);
-        store_at<DT, N>(x, t.line(a.dx, up_x, i), f);
+        store_at<DT, N>(x, off_x + i * t.next(up_x), f);
     }
 }
 
-// pixels of a thread: four 16-bit ones while a thread may have 256 registers (it takes 130 to 230), else two
-constexpr int bwd_pixels(int dtype, int threads) { return dtype == 0 || threads == 1024 ? 2 : 4; }
+// pixels of a thread: four while it may have 256 registers, else two
+constexpr int bwd_pixels(int threads) { return threads == 1024 ? 2 : 4; }
 
 // Backwards: a workgroup walks the tiles gridDim.x apart and keeps its threads' sums for dgamma and dbeta in registers until the end, where they go to the
 // workgroup's copy of the scratch, or to dgamma and dbeta themselves if there is one workgroup.
 template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(NormBwdArgs a, long tiles, long row)
 {
-    constexpr int V = bwd_pixels(DT, T);
+    constexpr int V = bwd_pixels(T);
     extern __shared__ __align__(16) float part[];
     Tile<DT, LAYOUT, P, V> t(a.plane, row, tiles, a.c);
     const uint64_t counter = ADD ? a.drop.base() : 0;
     const int c0 = 8 * t.octet(), left = a.c - c0;
     float gamma[8], dg[8], db[8];
+    octet_values(a.gamma, c0, left, 1.f, gamma);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        gamma[j] = j >= left ? 0.f : a.gamma ? a.gamma[c0 + j] : 1.f;       // what does not count adds nothing to the sums over channels
+        gamma[j] = j < left ? gamma[j] : 0.f;           // what does not count adds nothing to the sums over channels
         dg[j] = db[j] = 0.f;
     }
     int half = 0;
-    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (long tile = neighbour(); tile < tiles; tile += gridDim.x) {
         t.go(tile);
         typename Tile<DT, LAYOUT, P, V>::Octet vy, vs;
         t.load(a.dy, t.oct0, vy);
@@ -109,10 +111,16 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         float *out = alone ? (which ? a.dbeta : a.dgamma) : a.scratch + (blockIdx.x * 2L + which) * cp;
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float v = sum_lanes<P>(which ? db[j] : dg[j]);
-            if (out && t.lane == 0 && j < left) out[c0 + j] = v;
+        for (int j = 0; j < 8; ++j) v[j] = sum_lanes<P>(which ? +db[j] : +dg[j]);
+        if (!out || t.lane != 0) continue;
+        if (left >= 8) {
+            store_at<0, 8>(reinterpret_cast<dst_t>(out), 4 * c0, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < left) out[c0 + j] = v[j];
         }
     }
 }
@@ -125,7 +133,7 @@ template <int DT, int LAYOUT, int P, int V> __global__ __launch_bounds__(1024) v
     const uint64_t counter = a.drop.base();
     const int last = (a.c + 7) / 8, octs = blockDim.x / P;
     int half = 0;
-    for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (long tile = neighbour(); tile < tiles; tile += gridDim.x) {
         t.go(tile);
         float mean[V], rstd[V], sums[2][V] = {}, mg[V], mgh[V], gamma[8];
         t.statistics(a.mean, mean);
@@ -135,8 +143,9 @@ template <int DT, int LAYOUT, int P, int V> __global__ __launch_bounds__(1024) v
             t.load(a.dy, o0, vy);
             t.load(a.s, o0, vs);
             const int c0 = 8 * (o0 + t.delta);
+            octet_values(a.gamma, c0, a.c - c0, 1.f, gamma);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) gamma[j] = c0 + j >= a.c ? 0.f : a.gamma ? a.gamma[c0 + j] : 1.f;
+            for (int j = 0; j < 8; ++j) gamma[j] = c0 + j < a.c ? gamma[j] : 0.f;
         };
         for (int o0 = t.oct0; o0 < last; o0 += octs) {
             take(o0);
@@ -208,8 +217,8 @@ int norm_planes_bwd_copies(const NormSpan &s)
 {
     int copies = 16;
     if (s.layout == OCTETS || s.plane >= 4)
-        pick_planes(s.c, [&](auto p, auto t, int threads) {
-            copies = (int)std::min<long>(s.n * tiles_of_image(s, p() * bwd_pixels(s.dtype, t())), 256 * std::max(1, 1024 / threads));
+        pick_planes<true>(s.c, [&](auto p, auto t, int threads) {
+            copies = (int)std::min<long>(s.n * tiles_of_image(s, p() * bwd_pixels(t())), 256 * std::max(1, 1024 / threads));
         });
     return copies;
 }
@@ -221,10 +230,10 @@ hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t 
     pick_type(a, [&](auto dt, auto layout) {
         bool done = false;
         if (layout() == OCTETS || a.plane >= 4)
-            pick_planes(a.c, [&](auto p, auto t, int threads) {
+            pick_planes<true>(a.c, [&](auto p, auto t, int threads) {
                 if (!fits(p())) return;
-                const long row = tiles_of_image(a, p() * bwd_pixels(dt(), t())), tiles = a.n * row;
-                const size_t lds = part_bytes(2, p(), bwd_pixels(dt(), t()), threads);
+                const long row = tiles_of_image(a, p() * bwd_pixels(t())), tiles = a.n * row;
+                const size_t lds = part_bytes(2, p(), bwd_pixels(t()), threads);
                 if (adds) norm_planes_bwd_kernel<dt(), layout(), p(), t(), true><<<copies, threads, lds, stream>>>(a, tiles, row);
                 else norm_planes_bwd_kernel<dt(), layout(), p(), t(), false><<<copies, threads, lds, stream>>>(a, tiles, row);
                 if (sums && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);

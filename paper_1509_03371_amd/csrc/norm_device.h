@@ -110,6 +110,32 @@ template <int P> __device__ __forceinline__ float sum_over_groups(float v)
     return v;
 }
 
+// A stretch of a line, V elements a lane in whole vectors.  Lanes whose V would reach over the stretch's end take its last V instead; what two lanes hold is
+// computed alike and stored twice, by lanes of one wave, after both have read it (so results may go to the operands' place).  A stretch of the line's
+// last 1 to V - 1 elements takes V, and the one in front of it ends so much earlier: no element is in two stretches.
+template <int V> struct Stretch {
+    long start;                                         // its first element: equal in all lanes
+    uint32_t length, at;                                // the lane's first, behind that
+    __device__ __forceinline__ Stretch() {}
+    // the stretch of `span` from element `first` on, of a line of `count` >= V; at: lane number * V
+    __device__ __forceinline__ Stretch(long first, int span, long count, uint32_t mine)
+    {
+        const long end = first + span;
+        start = first < count - V ? first : count - V;
+        length = (uint32_t)((end >= count ? count : end < count - V ? end : count - V) - start);
+        at = mine < length - V ? mine : length - V;
+    }
+    __device__ __forceinline__ bool empty(uint32_t mine) const { return mine >= length; }
+};
+
+// This workgroup's number among gridDim.x such that neighbours run on one XCD: workgroups go to the eight XCDs in turn, each has an L2 of its own, and lines
+// of maps begin anywhere, so neighbouring tiles share the cache lines at their ends.
+__device__ __forceinline__ unsigned neighbour()
+{
+    const unsigned xcd = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
+    return xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+}
+
 // workgroups for so much work: up to 2^21 (a grid may have 2^32 - 1 threads), which then walk it
 inline unsigned norm_blocks(long work, long each)
 {

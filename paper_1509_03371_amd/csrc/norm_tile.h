@@ -6,6 +6,23 @@
 
 namespace sk {
 
+// the values of channels c0 .. c0 + 7 (left: how many there are; the others, and all of a null pointer, are `without`)
+__device__ __forceinline__ void octet_values(const float *p, int c0, int left, float without, float (&f)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = without;
+    if (!p) return;
+    if (left >= 8) {
+        const line_t<0, 8> v = *reinterpret_cast<const line_t<0, 8> *>(p + c0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < left) f[j] = p[c0 + j];
+    }
+}
+
 // Where a thread stands.  A workgroup takes P * V pixels of one image and all channels (or as many octets at a time as it has threads / P): thread t the
 // V pixels of lane t % P in the eight channels of octet t / P.
 template <int DT, int LAYOUT, int P, int V> struct Tile {
@@ -31,8 +48,7 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
     const int c;
     const int lane, delta, oct0;                        // octet: oct0 of the wave's first lane + delta
     long b, start;                                      // image, first pixel of the tile
-    long from;                                          // MAPS: first pixel that the wave reads
-    uint32_t px;                                        // ... and where this lane's begin, behind that
+    uint32_t length, px;                                // MAPS: its pixels, and where this lane's begin
 
     __device__ __forceinline__ Tile(long plane_, long row_, long tiles, int c_)
         : plane(plane_), row(row_), narrow(tiles < (1L << 32)), c(c_), lane(threadIdx.x % P), delta((threadIdx.x & 63) / P),
@@ -45,13 +61,11 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
         b = narrow ? (long)((uint32_t)tile / (uint32_t)row) : tile / row;
         start = (tile - b * row) * (P * V);
         if (LAYOUT == MAPS) {
-            // Lanes whose pixels would reach over the plane's end take its last V instead: each load and store is whole.  Pixels that two lanes hold
-            // are computed alike and stored twice; both lanes are of one wave, so both have read before either writes.
-            from = start < plane - V ? start : plane - V;
-            const long mine = start + V * lane < plane - V ? start + V * lane : plane - V;
-            px = (uint32_t)(mine - from);
+            const Stretch<V> s(start, P * V, plane, V * lane);
+            start = s.start;
+            length = s.length;
+            px = s.at;
         } else {
-            from = start;
             px = lane;
         }
     }
@@ -62,18 +76,18 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
         const uint32_t last = (uint32_t)std::min<long>(plane - 1 - start, P * V);
         return std::min<uint32_t>(v * P + lane, last);
     }
-    __device__ __forceinline__ long pixel(int v) const { return from + behind(v); }
+    __device__ __forceinline__ long pixel(int v) const { return start + behind(v); }
     __device__ __forceinline__ long position(int v) const { return b * plane + pixel(v); }
     __device__ __forceinline__ bool inside(int v) const { return LAYOUT == MAPS || start + v * P + lane < plane; }
     // ... and does it count here in sums over pixels?
-    __device__ __forceinline__ bool own(int v) const { return LAYOUT == MAPS ? pixel(v) >= start + V * lane : inside(v); }
-    __device__ __forceinline__ bool stores() const { return LAYOUT != MAPS || start + V * lane < plane; }
+    __device__ __forceinline__ bool own(int v) const { return LAYOUT == MAPS ? px + v >= (uint32_t)(V * lane) : inside(v); }
+    __device__ __forceinline__ bool stores() const { return LAYOUT != MAPS || (uint32_t)(V * lane) < length; }
     // Every thread loads, whole vectors and without a branch.  Channels behind the last repeat the last one's address, threads without an octet the first
     // of their wave; what they hold must not count.  o0: the wave's first octet, which has channels.
     __device__ __forceinline__ int channels(int o0) const { return c - 8 * (o0 + delta); }       // of this thread's octet: 8 and more = all
     __device__ __forceinline__ long base(const NormView &w, int o0) const
     {
-        return S * (LAYOUT == MAPS ? b * w.sn + 8L * o0 * w.sc + from : b * w.sn + o0 * w.sc + 8 * start);
+        return S * (LAYOUT == MAPS ? b * w.sn + 8L * o0 * w.sc + start : b * w.sn + o0 * w.sc + 8 * start);
     }
     // from one channel (MAPS) or octet to the next, in bytes.  Opaque, or the compiler keeps eight multiples of it for every operand across the loop
     // over tiles, in more registers than the scalar unit has.
@@ -98,21 +112,19 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
             for (int v = 0; v < V; ++v) raw.unit[v].load(p, off + 8 * S * behind(v));
         }
     }
-    // a channel's line (MAPS) or a pixel's unit of an octet that has channels
-    __device__ __forceinline__ uint32_t line(const NormView &w, uint32_t up, int i) const
-    {
-        return LAYOUT == MAPS ? up * (8 * delta + i) + S * px : up * delta + 8 * S * (i * P + lane);
-    }
+    // where a channel's line (MAPS) or a pixel's unit of an octet that has channels lies behind base(): first + i * (this)
+    __device__ __forceinline__ uint32_t first(uint32_t up) const { return LAYOUT == MAPS ? 8 * up * delta + S * px : up * delta + 8 * S * lane; }
+    __device__ __forceinline__ static uint32_t next(uint32_t up) { return LAYOUT == MAPS ? up : 8 * S * P; }
     __device__ __forceinline__ void store(const NormView &w, int o0, const float (&f)[8][V]) const
     {
         const int left = channels(o0);
         if (left <= 0 || !stores()) return;
         const dst_t p = static_cast<dst_t>(w.p) + base(w, o0);
-        const uint32_t up = step(w);
+        const uint32_t up = step(w), off = first(up);
         if (LAYOUT == MAPS) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j < left) store_at<DT, V>(p, line(w, up, j), f[j]);
+                if (j < left) store_at<DT, V>(p, off + j * up, f[j]);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v)
@@ -120,7 +132,7 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
                     float u[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) u[j] = j < left ? f[j][v] : 0.f;
-                    store_at<DT, 8>(p, line(w, up, v), u);
+                    store_at<DT, 8>(p, off + v * next(up), u);
                 }
         }
     }
@@ -207,11 +219,8 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
         if (left <= 0) return;
         if (ADD && a.sum.p) store(a.sum, o0, s);
         float gamma[8], beta[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            gamma[j] = a.gamma && j < left ? a.gamma[c0 + j] : 1.f;
-            beta[j] = a.beta && j < left ? a.beta[c0 + j] : 0.f;
-        }
+        octet_values(a.gamma, c0, left, 1.f, gamma);
+        octet_values(a.beta, c0, left, 0.f, beta);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -227,7 +236,7 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
     {
         if (LAYOUT == MAPS) {
             Words<0, V> u;
-            u.load(reinterpret_cast<src_t>(p + b * plane + from), 4 * px);
+            u.load(reinterpret_cast<src_t>(p + b * plane + start), 4 * px);
 #pragma unroll
             for (int v = 0; v < V; ++v) f[v] = u[v];
         } else {
@@ -266,20 +275,21 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
                 p[(n * waves + wave) * P + lane] = u;
             }
         __syncthreads();
+        // the 64 / P octets of a wave share the waves' sums out among them
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            Sums u = p[n * waves * P + lane];
-            for (int i = 1; i < waves; ++i) u += p[(n * waves + i) * P + lane];
+            Sums u{};
+            for (int i = delta; i < waves; i += 64 / P) u += p[(n * waves + i) * P + lane];
 #pragma unroll
-            for (int v = 0; v < V; ++v) s[n][v] = u[v];
+            for (int v = 0; v < V; ++v) s[n][v] = sum_over_groups<P>(u[v]);
         }
     }
 };
 
 template <int N> using num = std::integral_constant<int, N>;
 
-// f(P, T) and the threads of a workgroup that holds c channels; false: more than it can
-template <class F> bool pick_planes(int c, F f)
+// f(P, T) and the threads of a workgroup that holds c channels; false: more than it can.  BACK: backwards
+template <bool BACK, class F> bool pick_planes(int c, F f)
 {
     const int octs = (c + 7) / 8;
     auto go = [&](auto p, auto t) {
@@ -289,7 +299,7 @@ template <class F> bool pick_planes(int c, F f)
     if (octs <= 4) return go(num<64>{}, num<256>{});
     if (octs <= 8) return go(num<32>{}, num<256>{});
     if (octs <= 16) return go(num<16>{}, num<256>{});
-    if (octs <= 64) return go(num<16>{}, num<1024>{});
+    if (octs <= 64) return go(num<BACK ? 8 : 16>{}, num<BACK ? 512 : 1024>{});
     if (octs <= 128) return go(num<8>{}, num<1024>{});
     if (octs <= 256) return go(num<4>{}, num<1024>{});
     return false;
