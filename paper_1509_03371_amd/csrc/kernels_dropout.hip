@@ -54,25 +54,16 @@ template <int DT, int V> __global__ __launch_bounds__(256) void dropout_maps_ker
         Words<DT, V> v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j].load(x + std::min(j, left - 1) * up_x, off);        // (channels behind the last repeat it)
-        uint32_t bits = 0;
-        auto draw = [&](auto i) {
-            if constexpr (i() < V) {
-                uint32_t w[4];
-                mask_words(w, a.drop, counter, (uint64_t)(b * a.plane + from + px + i()), o);
-                bits |= keep_bits<8 * i()>(w, a.drop);
-            }
-        };
-        draw(std::integral_constant<int, 0>{});
-        draw(std::integral_constant<int, 1>{});
-        draw(std::integral_constant<int, 2>{});
-        draw(std::integral_constant<int, 3>{});
+        uint32_t w[V][4];
+#pragma unroll
+        for (int i = 0; i < V; ++i) mask_words(w[i], a.drop, counter, (uint64_t)(b * a.plane + from + px + i), o);
         src_t r = reinterpret_cast<src_t>(static_cast<const E *>(a.relu_src.p) + b * a.relu_src.sn + 8L * o * a.relu_src.sc + from);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < left) {
                 float f[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = kept(v[j][i], bits, 8 * i + j, a.drop);
+                for (int i = 0; i < V; ++i) f[i] = dropped(v[j][i], w[i], j, a.drop);
                 if (a.relu_src.p) {
                     Words<DT, V> u;
                     u.load(r + j * up_r, off);

@@ -15,13 +15,18 @@ __device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, c
     const int left = t.channels(o0);
     if (left <= 0 || !t.stores()) return;
     const bool drops = ADD && a.drop.thresh && a.dx.p;
-    const uint32_t bits = drops ? t.mask(a.drop, counter, o0 + t.delta) : ~0u;
-    auto gradient = [&](int j, int v) {
-        const float h = (vs.at(j, v) - mean[v]) * rstd[v];
-        return rstd[v] * (vy.at(j, v) * gamma[j] - mg[v] - h * mgh[v]);
-    };
+    uint32_t w[V][4];
+    if (drops) t.draw(a.drop, counter, o0 + t.delta, w);
+    // rstd (gamma dy - mg - h mgh) with h = (s - mean) rstd, as dy (gamma rstd) - mg rstd - (s - mean) (mgh rstd^2)
+    float mr[V], mr2[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        mr[v] = mg[v] * rstd[v];
+        mr2[v] = mgh[v] * rstd[v] * rstd[v];
+    }
+    auto gradient = [&](int j, int v) { return vy.at(j, v) * (gamma[j] * rstd[v]) - mr[v] - (vs.at(j, v) - mean[v]) * mr2[v]; };
     auto to_x = [&](int j, int v, float f) {
-        if (drops) f = kept(f, bits, 8 * v + j, a.drop);
+        if (drops) f = dropped(f, w[v], j, a.drop);
         return a.relu_x && !(vs.at(j, v) > 0.f) ? 0.f : f;
     };
     // a line at a time, each behind a branch of its own: together the values of all lines are more than the registers hold
@@ -79,18 +84,21 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
         float mean[V], rstd[V], sums[2][V] = {};
         t.statistics(a.mean, mean);
         t.statistics(a.rstd, rstd);
-        bool own[V];
+        float once[V], r_once[V];                       // 1 and rstd, 0 where another lane holds the pixel
 #pragma unroll
-        for (int v = 0; v < V; ++v) own[v] = t.own(v);
+        for (int v = 0; v < V; ++v) {
+            once[v] = t.own(v) ? 1.f : 0.f;
+            r_once[v] = once[v] * rstd[v];
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float h = (vs.at(j, v) - mean[v]) * rstd[v], y = vy.at(j, v), g = y * gamma[j], mine = own[v] ? y : 0.f;
+                const float d = vs.at(j, v) - mean[v], y = vy.at(j, v), g = y * gamma[j];
                 sums[0][v] += g;
-                sums[1][v] += g * h;
-                dg[j] += mine * h;
-                db[j] += mine;
+                sums[1][v] += g * d;
+                dg[j] += y * r_once[v] * d;
+                db[j] += y * once[v];
             }
         t.template total<2>(sums, part, half);
         if (!a.dx.p && !a.dresidual.p) continue;
@@ -98,10 +106,12 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             mg[v] = sums[0][v] / (float)a.c;
-            mgh[v] = sums[1][v] / (float)a.c;
+            mgh[v] = sums[1][v] * rstd[v] / (float)a.c;
         }
-        vy.forget();
-        vs.forget();
+        if (T == 1024) {
+            vy.forget();
+            vs.forget();
+        }
         put_gradients<ADD>(t, a, counter, t.oct0, vy, vs, gamma, mean, rstd, mg, mgh);
     }
     if (!a.dgamma && !a.dbeta) return;
@@ -218,7 +228,7 @@ int norm_planes_bwd_copies(const NormSpan &s)
     int copies = 16;
     if (s.layout == OCTETS || s.plane >= 4)
         pick_planes<true>(s.c, [&](auto p, auto t, int threads) {
-            copies = (int)std::min<long>(s.n * tiles_of_image(s, p() * bwd_pixels(t())), 256 * std::max(1, 1024 / threads));
+            copies = (int)std::min<long>(s.n * tiles_of_image(s, p() * bwd_pixels(t())), 256 * std::max(1, (t() == 1024 ? 16 : 8) / (threads / 64)));
         });
     return copies;
 }

@@ -136,22 +136,11 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
                 }
         }
     }
-    // bit 8 * v + j: is channel j of pixel v kept?
-    __device__ __forceinline__ uint32_t mask(const DropMask &d, uint64_t counter, int o) const
+    // the numbers of an octet's channels at each pixel
+    __device__ __forceinline__ void draw(const DropMask &d, uint64_t counter, int o, uint32_t (&w)[V][4]) const
     {
-        uint32_t bits = 0;
-        auto add = [&](auto v) {
-            if constexpr (v() < V) {
-                uint32_t w[4];
-                mask_words(w, d, counter, (uint64_t)position(v()), o);
-                bits |= keep_bits<8 * v()>(w, d);
-            }
-        };
-        add(std::integral_constant<int, 0>{});
-        add(std::integral_constant<int, 1>{});
-        add(std::integral_constant<int, 2>{});
-        add(std::integral_constant<int, 3>{});
-        return bits;
+#pragma unroll
+        for (int v = 0; v < V; ++v) mask_words(w[v], d, counter, (uint64_t)position(v), o);
     }
     // s = x, or residual + dropout(x), of an octet
     template <bool ADD> __device__ __forceinline__ void values(const NormArgs &a, uint64_t counter, int o0, float (&s)[8][V]) const
@@ -164,11 +153,12 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
 #pragma unroll
             for (int v = 0; v < V; ++v) s[j][v] = x.at(j, v);
         if (ADD && a.drop.thresh) {
-            const uint32_t bits = mask(a.drop, counter, o0 + delta);
+            uint32_t w[V][4];
+            draw(a.drop, counter, o0 + delta, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int v = 0; v < V; ++v) s[j][v] = kept(s[j][v], bits, 8 * v + j, a.drop);
+                for (int v = 0; v < V; ++v) s[j][v] = dropped(s[j][v], w[v], j, a.drop);
         }
         if (ADD && a.residual.p)
 #pragma unroll

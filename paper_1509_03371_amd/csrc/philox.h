@@ -5,17 +5,20 @@
 
 namespace sk {
 
+// a ^ b ^ c in one instruction (the compiler takes two)
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+
 // Philox4x32-10 (J. Salmon, M. Moraes, R. Dror, D. Shaw: Parallel random numbers: as easy as 1, 2, 3; SC 2011): ten rounds
 // of two 32 x 32 -> 64 bit products on a 128-bit counter, under a 64-bit key.  Every counter value gives four words that do
 // not depend on any other call, so a mask can be made again wherever it is needed and is never stored.
-__host__ __device__ __forceinline__ void philox4x32(uint32_t (&w)[4], uint32_t k0, uint32_t k1)
+__device__ __forceinline__ void philox4x32(uint32_t (&w)[4], uint32_t k0, uint32_t k1)
 {
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)0xD2511F53u * w[0], b = (uint64_t)0xCD9E8D57u * w[2];
-        w[0] = (uint32_t)(b >> 32) ^ w[1] ^ k0;
+        w[0] = xor3((uint32_t)(b >> 32), w[1], k0);
         w[1] = (uint32_t)b;
-        w[2] = (uint32_t)(a >> 32) ^ w[3] ^ k1;
+        w[2] = xor3((uint32_t)(a >> 32), w[3], k1);
         w[3] = (uint32_t)a;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
@@ -48,25 +51,6 @@ __device__ __forceinline__ float dropped(float v, const uint32_t (&w)[4], int j,
 {
     const uint32_t u = (j & 1) ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu;
     return u >= m.thresh ? v * m.scale : 0.f;
-}
-
-// the mask of an octet as bits, channel j at bit FIRST + j (dropped: 0): one register for four positions
-template <int FIRST> __device__ __forceinline__ uint32_t keep_bits(const uint32_t (&w)[4], const DropMask &m)
-{
-    uint32_t bits = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t u = (j & 1) ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu;
-        bits |= (u >= m.thresh ? 1u : 0u) << (FIRST + j);
-    }
-    return bits;
-}
-
-// v scaled where the bit is set, else zero (of NaN and infinity too)
-__device__ __forceinline__ float kept(float v, uint32_t bits, int bit, const DropMask &m)
-{
-    const int all = (int)(bits << (31 - bit)) >> 31;     // 0 or -1
-    return __uint_as_float(__float_as_uint(v * m.scale) & (uint32_t)all);
 }
 
 }  // namespace sk
