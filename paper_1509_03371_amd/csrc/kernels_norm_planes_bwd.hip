@@ -126,7 +126,7 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
         for (int j = 0; j < 8; ++j) v[j] = sum_lanes<P>(which ? +db[j] : +dg[j]);
         if (!out || t.lane != 0) continue;
         if (left >= 8) {
-            store_at<0, 8>(reinterpret_cast<dst_t>(out), 4 * c0, v);
+            *reinterpret_cast<line_t<0, 8> *>(out + c0) = packed<0, 8>(v);
         } else {
 #pragma unroll
             for (int j = 0; j < 7; ++j)

@@ -289,9 +289,21 @@ __device__ __forceinline__ void put_gradients(const Row<DT, G> &r, const NormBwd
     r.store(a.dx, row0, k, t);
 }
 
+// sums of channels c0 .. c0 + 7 of c, which the reduction reads
+__device__ __forceinline__ void put_values(float *out, int c, int c0, const float (&f)[8])
+{
+    if (c0 + 8 <= c) {
+        *reinterpret_cast<line_t<0, 8> *>(out + c0) = packed<0, 8>(f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (c0 + j < c) out[c0 + j] = f[j];
+    }
+}
+
 // Backwards: a workgroup walks rows gridDim.x * T / G apart and keeps its lanes' sums for dgamma and dbeta in registers until the end, where they
 // go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta themselves if there is one workgroup.
-template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T) void norm_rows_bwd_kernel(NormBwdArgs a)
+template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T, 4) void norm_rows_bwd_kernel(NormBwdArgs a)
 {
     constexpr int W = T / 64;
     __shared__ float part[G > 64 ? 4 * W : 1];
@@ -375,11 +387,9 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T)
     auto put = [&](const float (&acc)[K][8], float *own, int which) {
         float *out = alone ? own : a.scratch + (blockIdx.x * 2L + which) * cp;
         if (G == T) {                                   // every channel belongs to one lane of the workgroup
-            const Row<0, G> f(a.c);
-            const NormView v{out, 0, 0};
             if (out)
 #pragma unroll
-                for (int k = 0; k < K; ++k) f.store(v, 0, k, acc[k]);
+                for (int k = 0; k < K; ++k) put_values(out, a.c, r.channel(k), acc[k]);
             return;
         }
         // rows of one wave first, then the waves in order
@@ -469,9 +479,8 @@ template <int DT> __global__ __launch_bounds__(1024) void norm_long_rows_wgrad_k
                 db[j] += vy[j];
             }
         }
-        const Row<0, 1024> f(a.c);
-        f.store(NormView{a.scratch + blockIdx.y * 2L * cp, 0, 0}, 0, k, dg);
-        f.store(NormView{a.scratch + (blockIdx.y * 2L + 1) * cp, 0, 0}, 0, k, db);
+        put_values(a.scratch + blockIdx.y * 2L * cp, a.c, r.channel(k), dg);
+        put_values(a.scratch + (blockIdx.y * 2L + 1) * cp, a.c, r.channel(k), db);
     }
 }
 
