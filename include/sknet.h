@@ -48,7 +48,7 @@ typedef enum {
  * images, probabilities, labels, weights and gradients cross the ABI as fp32 / int32. */
 typedef enum { SK_F32 = 0, SK_BF16 = 1, SK_F16 = 2 } sk_dtype;
 
-typedef enum { SK_CONV = 0, SK_MAXPOOL = 1 } sk_kind;
+typedef enum { SK_CONV = 0, SK_MAXPOOL = 1, SK_LAYERNORM = 2, SK_DROPOUT = 3 } sk_kind;
 
 /* One layer of an SK net, in the terms of the paper's configuration tables (Section 3.3.2):
  *   SK_CONV    : f_out = c_out maps, kernel k x k, kernel stride d, s must be 1; relu != 0 applies
@@ -56,6 +56,11 @@ typedef enum { SK_CONV = 0, SK_MAXPOOL = 1 } sk_kind;
  *                (Section 5.2.1; cross-correlation, no padding).
  *   SK_MAXPOOL : kernel k x k, kernel stride d, layer stride s (1 for SK pooling; s = k with d = 1
  *                for an ordinary down-sampling pool).  c_out and relu are ignored.
+ *   SK_LAYERNORM: per image and pixel, (x - mean) / sqrt(variance + 1e-5) over the maps, times gamma plus beta per map (sknet_set_norm);
+ *                relu != 0 applies max(0, .).  k = d = s = 1; c_out is ignored.  2-D SK nets only.
+ *   SK_DROPOUT : a training plan's forward pass zeroes a sample with the rate c_out / 65536 and scales the others by the inverse of the rate kept
+ *                (sknet_set_dropout); an inference plan leaves the layer out.  k = d = s = 1, relu = 0.  2-D SK nets only.
+ * Neither looks at a neighbour, so a net with them still labels a pixel as its sliding window would.
  * Every layer with a kernel shrinks the map by (k-1)*d (Algorithm 1). */
 typedef struct {
     int32_t kind;  /* sk_kind */
@@ -130,6 +135,23 @@ sk_status sknet_conv_shape(const sknet_t *net, int32_t conv_idx, int32_t *shape4
  * the device copies are refreshed at once (synchronously). */
 sk_status sknet_set_weights(sknet_t *net, int32_t conv_idx, const float *w_host, const float *b_host);
 sk_status sknet_get_weights(sknet_t *net, int32_t conv_idx, float *w_host, float *b_host);
+
+/* SK_LAYERNORM layers, numbered in layer order: how many, over how many maps, and their fp32 gamma and beta [maps] (HOST; set: NULL = keep; get:
+ * either may be NULL; gamma starts as 1, beta as 0).  As sknet_set_weights / sknet_get_weights: before or after sknet_plan, synchronously.
+ * get_norm_grad: gradients of the last sknet_backward (SK_ESTATE without one); sknet_sgd_step updates gamma and beta by the rule of the weights. */
+sk_status sknet_num_norms(const sknet_t *net, int32_t *count);
+sk_status sknet_norm_size(const sknet_t *net, int32_t norm_idx, int32_t *maps);
+sk_status sknet_set_norm(sknet_t *net, int32_t norm_idx, const float *gamma_host, const float *beta_host);
+sk_status sknet_get_norm(sknet_t *net, int32_t norm_idx, float *gamma_host, float *beta_host);
+sk_status sknet_get_norm_grad(sknet_t *net, int32_t norm_idx, float *dgamma_host, float *dbeta_host);
+
+/* The masks of SK_DROPOUT layers: that of layer number l (0-based, of all layers) in the step-th forward pass on a training plan is the mask of
+ * sk_drop with this seed, offset = l * 2^40 + step, and positions image * height * width + pixel of the layer's maps.  sknet_forward on a
+ * training plan first adds one to the step, on the device (a recorded pass moves on at every replay), and sknet_backward makes the masks of the
+ * pass before it again.  Seed and step start as 0 and outlive plans; set both to repeat or resume a run (step < 2^40).  Both calls synchronise
+ * the stream of the last pass. */
+sk_status sknet_set_dropout(sknet_t *net, uint64_t seed, uint64_t step);
+sk_status sknet_get_dropout(sknet_t *net, uint64_t *seed, uint64_t *step);
 
 /* Fix the problem size: n images of h x w pixels, and allocate every workspace on the current
  * HIP device (hipMalloc).  pad != 0: the library mirror-pads the image by v so that the output
@@ -372,7 +394,8 @@ sk_status sknet3d_get_pool_argmax(sknet3d_t *net, int32_t pool_idx, int32_t *idx
 
 /* ---------------------------------------------------------------- operators on the caller's own tensors */
 
-/* Dropout and layer norm over the channels (maps) of each position, forwards and backwards, on tensors that the caller owns.
+/* Dropout and layer norm over the channels (maps) of each position, forwards and backwards, on tensors that the caller owns
+ * (as layers of a net: SK_LAYERNORM and SK_DROPOUT).
  *
  * A tensor has n * plane positions of c >= 1 channels in one of two orders:
  *   SK_ROWS: channel k of row r is element r*stride_n + k; plane must be 1 and stride_c is ignored;

@@ -5,6 +5,7 @@ TEST INFRASTRUCTURE ONLY.
 import numpy as np
 
 from . import layers as L
+from . import norm as N
 from .alg1 import context
 
 
@@ -14,18 +15,29 @@ def pad_amounts(v):
     return (v + 1) // 2, (v + 1) // 2, v // 2, v // 2
 
 
-def sknet_forward(image, sk_layers, weights, biases, pad=True, pad_mode=0, keep=False):
+def sknet_forward(image, sk_layers, weights, biases, pad=True, pad_mode=0, keep=False, norms=None, drop=None):
     """image[n,c,h,w] -> class probabilities [n,classes,h,w] (pad=True) for an SK net
     (laid out like the SK network configuration table of Section 3.3.2: conv SK + ReLU, max pool SK, ..., conv, softmax).
-    keep=True also returns every intermediate (for per-layer parity and for backward)."""
+    keep=True also returns every intermediate (for per-layer parity and for backward).
+    norms: (gamma, beta) of each layer norm, in order.  drop: (seed, step) of a training pass; None = inference, where dropout does nothing."""
     x = np.asarray(image, dtype=np.float64)
     if pad:
         t, l, b, r = pad_amounts(context(sk_layers))
         x = L.mirror_pad(x, t, l, b, r, pad_mode)
     acts, argmaxes = [x], []
-    wi = 0
-    for lay in sk_layers:
-        if lay["type"] == "conv":
+    wi = ni = 0
+    for li, lay in enumerate(sk_layers):
+        if lay["type"] == "norm":
+            x = N.layer_norm(x, *norms[ni])[0]
+            if lay.get("relu", False):
+                x = np.maximum(x, 0.0)
+            ni += 1
+            argmaxes.append(None)
+        elif lay["type"] == "dropout":
+            if drop is not None:
+                x = N.dropout(x, lay["p"], drop[0], li * 2 ** 40 + drop[1])
+            argmaxes.append(None)
+        elif lay["type"] == "conv":
             x = L.conv_sk(x, weights[wi], biases[wi], lay["d"], lay.get("relu", False))
             wi += 1
             argmaxes.append(None)
@@ -41,11 +53,12 @@ def sknet_forward(image, sk_layers, weights, biases, pad=True, pad_mode=0, keep=
     return prob
 
 
-def sknet_backward(sk_layers, weights, acts, argmaxes, labels, diffs=None):
+def sknet_backward(sk_layers, weights, acts, argmaxes, labels, diffs=None, norms=None, drop=None, norm_grads=None):
     """Exact gradient of the mean softmax loss w.r.t. every conv weight and bias.
     acts/argmaxes come from sknet_forward(keep=True).  Returns (loss, dW list, db list, d_input).
     diffs: an optional list that receives, per layer, the error map of that layer (the gradient of the
-    loss with respect to its output, after the layer's own ReLU derivative)."""
+    loss with respect to its output, after the layer's own ReLU derivative).
+    norms, drop as in sknet_forward; norm_grads: an optional list that receives (dgamma, dbeta) of each layer norm."""
     loss, g = L.softmax_loss(acts[-1], labels)
     if diffs is not None:
         diffs[:] = [None] * len(sk_layers)
@@ -55,7 +68,22 @@ def sknet_backward(sk_layers, weights, acts, argmaxes, labels, diffs=None):
     for li in range(len(sk_layers) - 1, -1, -1):
         lay = sk_layers[li]
         x_in, y_out = acts[li], acts[li + 1]
-        if lay["type"] == "conv":
+        if lay["type"] == "norm":
+            ni = sum(l["type"] == "norm" for l in sk_layers[:li])
+            if lay.get("relu", False):
+                g = L.relu_bwd(y_out, g)
+            if diffs is not None:
+                diffs[li] = g
+            _, mean, rstd = N.layer_norm(x_in, None, None)
+            g, dgamma, dbeta = N.layer_norm_bwd(g, x_in, mean, rstd, norms[ni][0])
+            if norm_grads is not None:
+                norm_grads.insert(0, (dgamma, dbeta))
+        elif lay["type"] == "dropout":
+            if diffs is not None:
+                diffs[li] = g
+            if drop is not None:
+                g = N.dropout(g, lay["p"], drop[0], li * 2 ** 40 + drop[1])
+        elif lay["type"] == "conv":
             if lay.get("relu", False):
                 g = L.relu_bwd(y_out, g)
             if diffs is not None:

@@ -18,7 +18,7 @@ if not os.path.exists(LIB_PATH):
 lib = C.CDLL(LIB_PATH)
 
 SK_F32, SK_BF16, SK_F16 = 0, 1, 2
-SK_CONV, SK_MAXPOOL = 0, 1
+SK_CONV, SK_MAXPOOL, SK_LAYERNORM, SK_DROPOUT = 0, 1, 2, 3
 SK_ROWS, SK_MAPS = 0, 1
 STATUS_NAMES = ["SK_OK", "SK_EINVAL", "SK_ESHAPE", "SK_ESTATE", "SK_ENOMEM", "SK_EDEVICE", "SK_EUNSUPPORTED"]
 DTYPES = {"f32": SK_F32, "bf16": SK_BF16, "f16": SK_F16}
@@ -107,6 +107,13 @@ _SIGS = {
     "sknet3d_get_grad": [_vp, _i32, _fp, _fp],
     "sknet3d_get_weights": [_vp, _i32, _fp, _fp],
     "sknet3d_get_pool_argmax": [_vp, _i32, _ip],
+    "sknet_num_norms": [_vp, _ip],
+    "sknet_norm_size": [_vp, _i32, _ip],
+    "sknet_set_norm": [_vp, _i32, _fp, _fp],
+    "sknet_get_norm": [_vp, _i32, _fp, _fp],
+    "sknet_get_norm_grad": [_vp, _i32, _fp, _fp],
+    "sknet_set_dropout": [_vp, C.c_uint64, C.c_uint64],
+    "sknet_get_dropout": [_vp, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)],
     "sknet_dropout": [_vp, _vp, _vp, _vp, _vp],
     "sknet_layer_norm": [_vp, _vp, _vp, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp, _vp, _vp],
     "sknet_layer_norm_workspace": [_vp, C.POINTER(C.c_uint64)],
@@ -157,13 +164,19 @@ def _dev_ptr(t, dtype, what):
 
 
 def layers_to_c(layers):
-    """[{'type': 'conv'|'pool', 'f_out', 'k', 'd', 's', 'relu'}] -> SkLayer array."""
+    """[{'type': 'conv'|'pool'|'norm'|'dropout', 'f_out', 'k', 'd', 's', 'relu', 'p'}] -> SkLayer array."""
     arr = (SkLayer * len(layers))()
     for i, l in enumerate(layers):
         if l["type"] == "conv":
             arr[i] = SkLayer(SK_CONV, l["f_out"], l["k"], l.get("d", 1), 1, int(l.get("relu", False)))
         elif l["type"] == "pool":
             arr[i] = SkLayer(SK_MAXPOOL, 0, l["k"], l.get("d", 1), l.get("s", 1), 0)
+        elif l["type"] == "norm":
+            arr[i] = SkLayer(SK_LAYERNORM, 0, 1, 1, 1, int(l.get("relu", False)))
+        elif l["type"] == "dropout":
+            if not 0.0 <= l["p"] <= 1.0:
+                raise ValueError("layer %d: the rate must be in [0, 1]" % i)
+            arr[i] = SkLayer(SK_DROPOUT, int(l["p"] * 65536.0 + 0.5), 1, 1, 1, 0)
         else:
             raise ValueError("unknown layer type %r" % (l["type"],))
     return arr
@@ -475,6 +488,48 @@ class SKNet:
         b = np.empty(shape[0], np.float32)
         _check(lib.sknet_get_weights(self._h, conv_idx, w.ctypes.data_as(_fp), b.ctypes.data_as(_fp)))
         return w, b
+
+    def num_norms(self):
+        c = C.c_int32()
+        _check(lib.sknet_num_norms(self._h, C.byref(c)))
+        return c.value
+
+    def norm_size(self, norm_idx):
+        c = C.c_int32()
+        _check(lib.sknet_norm_size(self._h, norm_idx, C.byref(c)))
+        return c.value
+
+    def set_norm(self, norm_idx, gamma=None, beta=None):
+        size = self.norm_size(norm_idx)
+        ptrs = []
+        for name, v in (("gammas", gamma), ("betas", beta)):
+            v, p = (None, None) if v is None else _f32(v)
+            if v is not None and v.shape != (size,):
+                raise ValueError("norm %d expects %d %s" % (norm_idx, size, name))
+            ptrs.append((v, p))
+        _check(lib.sknet_set_norm(self._h, norm_idx, ptrs[0][1], ptrs[1][1]))
+
+    def _norm_pair(self, fn, norm_idx):
+        gamma, beta = (np.empty(self.norm_size(norm_idx), np.float32) for _ in range(2))
+        _check(fn(self._h, norm_idx, gamma.ctypes.data_as(_fp), beta.ctypes.data_as(_fp)))
+        return gamma, beta
+
+    def get_norm(self, norm_idx):
+        return self._norm_pair(lib.sknet_get_norm, norm_idx)
+
+    def get_norm_grad(self, norm_idx):
+        return self._norm_pair(lib.sknet_get_norm_grad, norm_idx)
+
+    def set_dropout(self, seed, step=0):
+        if not 0 <= seed < 1 << 64 or step < 0:
+            raise ValueError("seed and step are unsigned")
+        _check(lib.sknet_set_dropout(self._h, seed, step))
+
+    def get_dropout(self):
+        """(seed, step): with them a later run continues the masks of this one."""
+        seed, step = C.c_uint64(), C.c_uint64()
+        _check(lib.sknet_get_dropout(self._h, C.byref(seed), C.byref(step)))
+        return seed.value, step.value
 
     def plan(self, n, h, w, pad=True, training=False, keep=False, fused_head=False):
         """mode 1 if training (3 with fused_head: the head and the loss as one kernel in each direction),

@@ -85,16 +85,20 @@ template <int DT> __global__ __launch_bounds__(256) void dropout_octets_kernel(D
         const int o = (int)(line % octs), left = a.c - 8 * o;
         if (first + threadIdx.x >= a.plane) continue;
         const uint32_t off = threadIdx.x * 8 * sizeof(E);
-        Words<DT, 8> x, r;
+        Words<DT, 8> x;
         x.load(reinterpret_cast<src_t>(static_cast<const E *>(a.x.p) + b * a.x.sn + o * a.x.sc + 8 * first), off);
-        if (a.relu_src.p) r.load(reinterpret_cast<src_t>(static_cast<const E *>(a.relu_src.p) + b * a.relu_src.sn + o * a.relu_src.sc + 8 * first), off);
         uint32_t w[4];
         mask_words(w, a.drop, counter, (uint64_t)(b * a.plane + first + threadIdx.x), o);
         float y[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            y[j] = dropped(x[j], w, j, a.drop);
-            if (j >= left || (a.relu_src.p && !(r[j] > 0.f))) y[j] = 0.f;
+        for (int j = 0; j < 8; ++j) y[j] = dropped(x[j], w, j, a.drop);
+        if (left < 8)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = j < left ? y[j] : 0.f;
+        if (a.relu_src.p) {
+            x.load(reinterpret_cast<src_t>(static_cast<const E *>(a.relu_src.p) + b * a.relu_src.sn + o * a.relu_src.sc + 8 * first), off);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = x[j] > 0.f ? y[j] : 0.f;
         }
         store_at<DT, 8>(reinterpret_cast<dst_t>(static_cast<E *>(a.y.p) + b * a.y.sn + o * a.y.sc + 8 * first), off, y);
     }

@@ -27,13 +27,12 @@ __device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, c
     auto gradient = [&](int j, int v) { return vy.at(j, v) * (gamma[j] * rstd[v]) - mr[v] - (vs.at(j, v) - mean[v]) * mr2[v]; };
     auto to_x = [&](int j, int v, float f) {
         if (drops) f = dropped(f, w[v], j, a.drop);
-        return a.relu_x && !(vs.at(j, v) > 0.f) ? 0.f : f;
+        if (a.relu_x) f = vs.at(j, v) > 0.f ? f : 0.f;
+        return f;
     };
     // a line at a time, each behind a branch of its own: together the values of all lines are more than the registers hold
-    auto lines = [&](const NormView &w) { return static_cast<dst_t>(w.p) + t.base(w, o0); };
-    const dst_t sum = ADD ? lines(a.dsum) : nullptr, residual = ADD ? lines(a.dresidual) : nullptr, x = lines(a.dx);
-    const uint32_t up_sum = ADD ? t.step(a.dsum) : 0, up_residual = ADD ? t.step(a.dresidual) : 0, up_x = t.step(a.dx);
-    const uint32_t off_sum = t.first(up_sum), off_residual = t.first(up_residual), off_x = t.first(up_x);
+    typedef typename Tile<DT, LAYOUT, P, V>::Lines Lines;
+    const Lines sum = ADD ? t.lines(a.dsum, o0) : Lines{}, residual = ADD ? t.lines(a.dresidual, o0) : Lines{}, x = t.lines(a.dx, o0);
     constexpr bool maps = LAYOUT == MAPS;
     constexpr int L = maps ? 8 : V, N = maps ? V : 8;   // lines, and elements of one
 #pragma unroll
@@ -44,15 +43,15 @@ __device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, c
         for (int e = 0; e < N; ++e) f[e] = maps ? gradient(i, e) : e < left ? gradient(e, i) : 0.f;
         if (ADD && a.dsum.p) {
             Words<DT, N> d;
-            d.load(sum, off_sum + i * t.next(up_sum));
+            d.load(sum.base(i), sum.offset(i));
 #pragma unroll
             for (int e = 0; e < N; ++e) f[e] += d[e];
         }
-        if (ADD && a.dresidual.p) store_at<DT, N>(residual, off_residual + i * t.next(up_residual), f);
+        if (ADD && a.dresidual.p) store_at<DT, N>(residual.base(i), residual.offset(i), f);
         if (ADD && !a.dx.p) continue;
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] = maps ? to_x(i, e, f[e]) : to_x(e, i, f[e]);
-        store_at<DT, N>(x, off_x + i * t.next(up_x), f);
+        store_at<DT, N>(x.base(i), x.offset(i), f);
     }
 }
 

@@ -91,9 +91,12 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
     }
     // from one channel (MAPS) or octet to the next, in bytes.  Opaque, or the compiler keeps eight multiples of it for every operand across the loop
     // over tiles, in more registers than the scalar unit has.
-    __device__ __forceinline__ uint32_t step(const NormView &w) const
+    // FAR: a wave's lanes are all in one octet, and the steps are added to the base, in 64 bits; else to the lanes' offsets, in 32.
+    static constexpr bool FAR = LAYOUT == MAPS && P == 64;
+    typedef typename std::conditional<FAR, long, uint32_t>::type Step;
+    __device__ __forceinline__ Step step(const NormView &w) const
     {
-        uint32_t v = S * (uint32_t)w.sc;
+        Step v = S * (Step)w.sc;
         asm volatile("" : "+s"(v));
         return v;
     }
@@ -101,8 +104,12 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
     {
         const int left = channels(o0);
         const src_t p = static_cast<src_t>(w.p) + base(w, o0);
-        const uint32_t up = step(w);
-        if constexpr (LAYOUT == MAPS) {
+        const Step up = step(w);
+        if constexpr (FAR) {
+            const int last = std::max(0, std::min(7, left - 1));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) raw.line[j].load(p + up * std::min(j, last), S * px);
+        } else if constexpr (LAYOUT == MAPS) {
             const uint32_t off = (left > 0 ? 8 * up * delta : 0) + S * px, last = up * std::max(0, std::min(7, left - 1));
 #pragma unroll
             for (int j = 0; j < 8; ++j) raw.line[j].load(p, off + std::min(up * j, last));
@@ -112,19 +119,29 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
             for (int v = 0; v < V; ++v) raw.unit[v].load(p, off + 8 * S * behind(v));
         }
     }
-    // where a channel's line (MAPS) or a pixel's unit of an octet that has channels lies behind base(): first + i * (this)
-    __device__ __forceinline__ uint32_t first(uint32_t up) const { return LAYOUT == MAPS ? 8 * up * delta + S * px : up * delta + 8 * S * lane; }
-    __device__ __forceinline__ static uint32_t next(uint32_t up) { return LAYOUT == MAPS ? up : 8 * S * P; }
+    // where line i of an octet that has channels lies: a channel's (MAPS) or a pixel's unit (OCTETS)
+    struct Lines {
+        dst_t p;
+        uint32_t off;
+        Step up;
+        __device__ __forceinline__ dst_t base(int i) const { return FAR ? p + i * up : p; }
+        __device__ __forceinline__ uint32_t offset(int i) const { return FAR ? off : off + i * (LAYOUT == MAPS ? (uint32_t)up : 8 * S * P); }
+    };
+    __device__ __forceinline__ Lines lines(const NormView &w, int o0) const
+    {
+        const Step up = step(w);
+        const uint32_t first = FAR ? S * px : LAYOUT == MAPS ? 8 * (uint32_t)up * delta + S * px : (uint32_t)up * delta + 8 * S * lane;
+        return {static_cast<dst_t>(w.p) + base(w, o0), first, up};
+    }
     __device__ __forceinline__ void store(const NormView &w, int o0, const float (&f)[8][V]) const
     {
         const int left = channels(o0);
         if (left <= 0 || !stores()) return;
-        const dst_t p = static_cast<dst_t>(w.p) + base(w, o0);
-        const uint32_t up = step(w), off = first(up);
+        const Lines at = lines(w, o0);
         if (LAYOUT == MAPS) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j < left) store_at<DT, V>(p, off + j * up, f[j]);
+                if (j < left) store_at<DT, V>(at.base(j), at.offset(j), f[j]);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v)
@@ -132,7 +149,7 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
                     float u[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) u[j] = j < left ? f[j][v] : 0.f;
-                    store_at<DT, 8>(p, off + v * next(up), u);
+                    store_at<DT, 8>(at.base(v), at.offset(v), u);
                 }
         }
     }
@@ -299,7 +316,7 @@ template <bool BACK, class F> bool pick_planes(int c, F f)
 inline bool spans(const NormSpan &s, int p, std::initializer_list<const NormView *> views)
 {
     for (const NormView *v : views)
-        if (v->p && (64 / p) * (s.layout == MAPS ? 8 : 1) * v->sc >= (1L << 30)) return false;      // elements of at most four bytes
+        if (p < 64 && v->p && (64 / p) * (s.layout == MAPS ? 8 : 1) * v->sc >= (1L << 30)) return false;      // elements of at most four bytes
     return true;
 }
 

@@ -2,10 +2,12 @@
 // per-layer launch sequences.  See include/sknet.h for the contract of every entry point.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <mutex>
 #include <new>
 
 #include "device_scope.h"
+#include "norm.h"
 #include "sk_host.h"
 
 using namespace skh;
@@ -42,8 +44,46 @@ sk_status static_scratch(float **out)
 }  // namespace
 
 // ================================================================================ SK-Net handle
+// One layer norm's parameters: fp32 master copy on the host and on the device, gradients and momentum, the statistics of a training pass.
+struct NormParams {
+    int c = 0;
+    std::vector<float> gamma, beta;
+    float *gamma_dev = nullptr, *beta_dev = nullptr, *dgamma = nullptr, *dbeta = nullptr, *vgamma = nullptr, *vbeta = nullptr;
+    float *mean = nullptr, *rstd = nullptr;
+    void release()
+    {
+        for (float **p : {&gamma_dev, &beta_dev, &dgamma, &dbeta, &vgamma, &vbeta, &mean, &rstd}) free_dev(*p);
+    }
+};
+constexpr float kNormEps = 1e-5f;
+
 struct sknet {
+    std::vector<sk_layer> all_layers; // as created
+    // What the plan runs: all of them for training; for inference without the dropout layers, which pass their maps on.  user_of: layer -> number among
+    // all_layers; maps_of: number among all_layers -> index of its output in dims and act.
     std::vector<sk_layer> layers;
+    std::vector<int> user_of, maps_of;
+    std::vector<NormParams> norms;
+    std::vector<int> norm_of_layer;   // layer -> norm index or -1
+    uint64_t drop_seed = 0, drop_step = 0;      // drop_step: while no plan holds the counter
+    uint64_t *step_dev = nullptr;     // training plans of nets with dropout: forward passes so far
+    void activate(bool training)
+    {
+        layers.clear(); user_of.clear(); maps_of.clear(); conv_of_layer.clear(); norm_of_layer.clear();
+        int nc = 0, nn = 0;
+        for (int i = 0; i < (int)all_layers.size(); ++i) {
+            const sk_layer &l = all_layers[i];
+            if (training || l.kind != SK_DROPOUT) {
+                layers.push_back(l);
+                user_of.push_back(i);
+                conv_of_layer.push_back(l.kind == SK_CONV ? nc++ : -1);
+                norm_of_layer.push_back(l.kind == SK_LAYERNORM ? nn++ : -1);
+            }
+            maps_of.push_back((int)layers.size());
+        }
+    }
+    // does layer li end in a ReLU?
+    bool relu_behind(int li) const { return li >= 0 && (layers[li].kind == SK_CONV || layers[li].kind == SK_LAYERNORM) && layers[li].relu; }
     int c_in = 0, n_classes = 0, dtype = 0, pad_mode = 0;
     std::vector<ConvParams> convs;
     std::vector<int> conv_of_layer;   // layer -> conv index or -1
@@ -105,6 +145,9 @@ struct sknet {
         c1_used = nullptr;
         head_pool = 0;
         for (auto &c : convs) release_conv(c);
+        for (auto &m : norms) m.release();
+        if (step_dev) (void)hipFree(step_dev);
+        step_dev = nullptr;
         planned = forward_done = backward_done = false;
     }
 };
@@ -112,11 +155,11 @@ struct sknet {
 namespace {
 
 // sizes of every map for an h x w image; shared by infer_shapes and plan
-sk_status infer(const sknet *net, int h, int w, int pad, std::vector<Dims> &dims, int *pt, int *pl)
+sk_status infer(const sknet *net, const std::vector<sk_layer> &layers, int h, int w, int pad, std::vector<Dims> &dims, int *pt, int *pl)
 {
     int v = 0;
     bool stride1 = true;
-    for (const auto &l : net->layers) {
+    for (const auto &l : layers) {
         v += (l.k - 1) * l.d;
         if (l.kind == SK_MAXPOOL && l.s != 1) stride1 = false;
     }
@@ -135,8 +178,8 @@ sk_status infer(const sknet *net, int h, int w, int pad, std::vector<Dims> &dims
     if (h < 1 || w < 1) return fail(SK_ESHAPE, "image size %dx%d", h, w);
     dims.clear();
     dims.push_back(cur);
-    for (size_t i = 0; i < net->layers.size(); ++i) {
-        const sk_layer &l = net->layers[i];
+    for (size_t i = 0; i < layers.size(); ++i) {
+        const sk_layer &l = layers[i];
         const int shrink = (l.k - 1) * l.d;
         if (l.kind == SK_CONV || l.s == 1) {
             cur.h -= shrink; cur.w -= shrink;
@@ -159,6 +202,36 @@ sk_status check_net(const sknet_t *net)
 {
     if (!net) return fail(SK_EINVAL, "null net handle");
     return SK_OK;
+}
+
+// the maps of an act or gradient buffer as an operand of the norm and dropout kernels: planes in fp32, octets in 16 bits
+sk::NormView maps_view(const sknet *net, void *p, const Dims &d)
+{
+    const long plane = (long)d.h * d.w, octets = (d.c + 7) / 8;
+    sk::NormView v;
+    v.p = p;
+    v.sc = net->half() ? 8 * plane : plane;
+    v.sn = net->half() ? 8 * octets * plane : d.c * plane;
+    return v;
+}
+
+void maps_span(const sknet *net, const Dims &d, sk::NormSpan *s)
+{
+    s->dtype = net->dtype;
+    s->layout = net->half() ? sk::OCTETS : sk::MAPS;
+    s->n = net->n; s->plane = (long)d.h * d.w; s->c = d.c;
+}
+
+// the mask of dropout layer li in the pass that the counter stands at
+sk::DropMask layer_mask(const sknet *net, int li)
+{
+    sk::DropMask m;
+    m.thresh = (uint32_t)net->layers[li].c_out;
+    m.scale = m.thresh >= 65536 ? 0.f : (float)(65536.0 / (65536.0 - m.thresh));
+    m.seed = net->drop_seed;
+    m.offset = (uint64_t)net->user_of[li] << 40;
+    m.step = net->step_dev;
+    return m;
 }
 
 // forward step `step`: 0 = pad/copy, 1..L = layers, L+1 = softmax; again: on what the last pass left behind
@@ -235,6 +308,23 @@ sk_status run_forward_step(sknet *net, int step_idx, hipStream_t stream, bool ag
                 sk::ConvF32Args a = conv_args(c, net->act[li], net->n, in, l.d, l.relu, net->act[li + 1], out);
                 SK_HIP(sk::launch_conv_f32(a, stream));
             }
+        } else if (l.kind == SK_LAYERNORM) {
+            const NormParams &m = net->norms[net->norm_of_layer[li]];
+            sk::NormArgs a{};
+            maps_span(net, in, &a);
+            a.x = maps_view(net, net->act[li], in);
+            a.y = maps_view(net, net->act[li + 1], out);
+            a.gamma = m.gamma_dev; a.beta = m.beta_dev; a.mean = m.mean; a.rstd = m.rstd;
+            a.eps = kNormEps;
+            a.relu = l.relu ? 1 : 0;
+            SK_HIP(sk::launch_layer_norm(a, stream));
+        } else if (l.kind == SK_DROPOUT) {
+            sk::DropoutArgs a{};
+            maps_span(net, in, &a);
+            a.x = maps_view(net, net->act[li], in);
+            a.y = maps_view(net, net->act[li + 1], out);
+            a.drop = layer_mask(net, li);
+            SK_HIP(sk::launch_dropout(a, stream));
         } else if (half) {
             SK_HIP(sk::launch_maxpool_h(net->act[li], net->act[li + 1], net->tap[li], net->dtype,
                                         (long)net->n * ((in.c + 7) / 8), in.h, in.w, out.h, out.w, l.k, l.d, l.s, stream));
@@ -342,7 +432,11 @@ sk_status sknet_create(const sk_layer *layers, int32_t n_layers, int32_t c_in, i
     for (int i = 0; i < n_layers; ++i) {
         const sk_layer &l = layers[i];
         sk_status bad = SK_OK;
-        if (l.kind != SK_CONV && l.kind != SK_MAXPOOL) bad = fail(SK_EINVAL, "layer %d: bad kind", i);
+        if (l.kind != SK_CONV && l.kind != SK_MAXPOOL && l.kind != SK_LAYERNORM && l.kind != SK_DROPOUT) bad = fail(SK_EINVAL, "layer %d: bad kind", i);
+        else if ((l.kind == SK_LAYERNORM || l.kind == SK_DROPOUT) && (l.k != 1 || l.d != 1 || l.s != 1))
+            bad = fail(SK_ESHAPE, "layer %d: layer norm and dropout need k = d = s = 1", i);
+        else if (l.kind == SK_DROPOUT && (l.c_out < 0 || l.c_out > 65536 || l.relu))
+            bad = fail(SK_EINVAL, "layer %d: dropout needs a rate c_out of 0 to 65536 (2^-16 each) and no relu", i);
         else if (l.k < 1 || l.d < 1) bad = fail(SK_ESHAPE, "layer %d: k and d must be >= 1", i);
         else if (l.k > 15) bad = fail(SK_EUNSUPPORTED, "layer %d: k > 15", i);
         else if (l.kind == SK_CONV && (l.s != 1 || l.c_out < 1)) bad = fail(SK_ESHAPE, "layer %d: conv needs s = 1 and c_out >= 1", i);
@@ -356,18 +450,26 @@ sk_status sknet_create(const sk_layer *layers, int32_t n_layers, int32_t c_in, i
             delete net;
             return bad;
         }
-        net->layers.push_back(l);
+        net->all_layers.push_back(l);
         if (l.kind == SK_CONV) {
             ConvParams c;
             c.c_in = maps; c.c_out = l.c_out; c.k = l.k;
             c.w.assign((size_t)c.wcount(), 0.f);
             c.b.assign((size_t)c.c_out, 0.f);
-            net->conv_of_layer.push_back((int)net->convs.size());
             net->convs.push_back(std::move(c));
             maps = l.c_out;
-        } else {
-            net->conv_of_layer.push_back(-1);
+        } else if (l.kind == SK_LAYERNORM) {
+            NormParams m;
+            m.c = maps;
+            m.gamma.assign((size_t)maps, 1.f);
+            m.beta.assign((size_t)maps, 0.f);
+            net->norms.push_back(std::move(m));
         }
+    }
+    net->activate(true);
+    if (net->layers.size() == std::count_if(layers, layers + n_layers, [](const sk_layer &l) { return l.kind == SK_DROPOUT; })) {
+        delete net;
+        return fail(SK_ESHAPE, "create: nothing but dropout layers");
     }
     if (maps != n_classes) {
         delete net;
@@ -402,7 +504,7 @@ sk_status sknet_infer_shapes(const sknet_t *net, int32_t h, int32_t w, int32_t p
     SK_TRY(check_net(net));
     if (!dims) return fail(SK_EINVAL, "infer_shapes: dims is null");
     std::vector<Dims> d;
-    SK_TRY(infer(net, h, w, pad, d, nullptr, nullptr));
+    SK_TRY(infer(net, net->all_layers, h, w, pad, d, nullptr, nullptr));
     for (size_t i = 0; i < d.size(); ++i) {
         dims[3 * i] = d[i].c; dims[3 * i + 1] = d[i].h; dims[3 * i + 2] = d[i].w;
     }
@@ -465,6 +567,123 @@ sk_status sknet_get_weights(sknet_t *net, int32_t conv_idx, float *w_host, float
     return SK_OK;
 }
 
+// a planned net's parameters and counter may have moved on the device: to the host's copies
+static sk_status save_state(sknet_t *net)
+{
+    for (int i = 0; i < (int)net->convs.size(); ++i) SK_TRY(sknet_get_weights(net, i, nullptr, nullptr));
+    for (int i = 0; i < (int)net->norms.size(); ++i) SK_TRY(sknet_get_norm(net, i, nullptr, nullptr));
+    uint64_t seed = 0, step = 0;
+    SK_TRY(sknet_get_dropout(net, &seed, &step));
+    net->drop_step = step;
+    return SK_OK;
+}
+
+static sk_status upload_norm(NormParams &m, hipStream_t stream)
+{
+    SK_HIP(hipMemcpyAsync(m.gamma_dev, m.gamma.data(), sizeof(float) * m.c, hipMemcpyHostToDevice, stream));
+    SK_HIP(hipMemcpyAsync(m.beta_dev, m.beta.data(), sizeof(float) * m.c, hipMemcpyHostToDevice, stream));
+    SK_HIP(hipStreamSynchronize(stream));
+    return SK_OK;
+}
+
+static sk_status alloc_norm(NormParams &m, bool training, long positions)
+{
+    m.release();
+    SK_TRY(alloc_f(&m.gamma_dev, m.c));
+    SK_TRY(alloc_f(&m.beta_dev, m.c));
+    if (training) {
+        for (float **p : {&m.dgamma, &m.dbeta, &m.vgamma, &m.vbeta}) SK_TRY(alloc_f(p, m.c));
+        SK_TRY(alloc_f(&m.mean, positions));
+        SK_TRY(alloc_f(&m.rstd, positions));
+        SK_HIP(hipMemset(m.vgamma, 0, sizeof(float) * m.c));
+        SK_HIP(hipMemset(m.vbeta, 0, sizeof(float) * m.c));
+    }
+    return upload_norm(m, nullptr);
+}
+
+static sk_status put_step(sknet_t *net)
+{
+    if (net->step_dev) SK_HIP(hipMemcpy(net->step_dev, &net->drop_step, sizeof(uint64_t), hipMemcpyHostToDevice));
+    return SK_OK;
+}
+
+sk_status sknet_num_norms(const sknet_t *net, int32_t *count)
+{
+    SK_TRY(check_net(net));
+    if (!count) return fail(SK_EINVAL, "num_norms: count is null");
+    *count = (int32_t)net->norms.size();
+    return SK_OK;
+}
+
+sk_status sknet_norm_size(const sknet_t *net, int32_t norm_idx, int32_t *maps)
+{
+    SK_TRY(check_net(net));
+    if (!maps || norm_idx < 0 || norm_idx >= (int)net->norms.size()) return fail(SK_EINVAL, "norm_size: bad arguments");
+    *maps = net->norms[norm_idx].c;
+    return SK_OK;
+}
+
+sk_status sknet_set_norm(sknet_t *net, int32_t norm_idx, const float *gamma_host, const float *beta_host)
+{
+    SK_TRY(check_net(net));
+    if (norm_idx < 0 || norm_idx >= (int)net->norms.size()) return fail(SK_EINVAL, "set_norm: bad index");
+    if (net->planned) SK_TRY(sknet_get_norm(net, norm_idx, nullptr, nullptr));     // what is not given keeps the device's value
+    NormParams &m = net->norms[norm_idx];
+    if (gamma_host) std::memcpy(m.gamma.data(), gamma_host, sizeof(float) * m.c);
+    if (beta_host) std::memcpy(m.beta.data(), beta_host, sizeof(float) * m.c);
+    return net->planned ? upload_norm(m, net->last_stream) : SK_OK;
+}
+
+sk_status sknet_get_norm(sknet_t *net, int32_t norm_idx, float *gamma_host, float *beta_host)
+{
+    SK_TRY(check_net(net));
+    if (norm_idx < 0 || norm_idx >= (int)net->norms.size()) return fail(SK_EINVAL, "get_norm: bad index");
+    NormParams &m = net->norms[norm_idx];
+    if (net->planned) {   // the device copy is the one SGD updates
+        SK_HIP(hipStreamSynchronize(net->last_stream));
+        SK_HIP(hipMemcpy(m.gamma.data(), m.gamma_dev, sizeof(float) * m.c, hipMemcpyDeviceToHost));
+        SK_HIP(hipMemcpy(m.beta.data(), m.beta_dev, sizeof(float) * m.c, hipMemcpyDeviceToHost));
+    }
+    if (gamma_host) std::memcpy(gamma_host, m.gamma.data(), sizeof(float) * m.c);
+    if (beta_host) std::memcpy(beta_host, m.beta.data(), sizeof(float) * m.c);
+    return SK_OK;
+}
+
+sk_status sknet_get_norm_grad(sknet_t *net, int32_t norm_idx, float *dgamma_host, float *dbeta_host)
+{
+    SK_TRY(check_net(net));
+    if (norm_idx < 0 || norm_idx >= (int)net->norms.size()) return fail(SK_EINVAL, "get_norm_grad: bad index");
+    if (!net->backward_done) return fail(SK_ESTATE, "get_norm_grad: no backward pass yet");
+    const NormParams &m = net->norms[norm_idx];
+    SK_HIP(hipStreamSynchronize(net->last_stream));
+    if (dgamma_host) SK_HIP(hipMemcpy(dgamma_host, m.dgamma, sizeof(float) * m.c, hipMemcpyDeviceToHost));
+    if (dbeta_host) SK_HIP(hipMemcpy(dbeta_host, m.dbeta, sizeof(float) * m.c, hipMemcpyDeviceToHost));
+    return SK_OK;
+}
+
+sk_status sknet_set_dropout(sknet_t *net, uint64_t seed, uint64_t step)
+{
+    SK_TRY(check_net(net));
+    if (step >> 40) return fail(SK_EINVAL, "set_dropout: the step must be below 2^40");
+    if (net->step_dev) SK_HIP(hipStreamSynchronize(net->last_stream));
+    net->drop_seed = seed;
+    net->drop_step = step;
+    return put_step(net);
+}
+
+sk_status sknet_get_dropout(sknet_t *net, uint64_t *seed, uint64_t *step)
+{
+    SK_TRY(check_net(net));
+    if (!seed || !step) return fail(SK_EINVAL, "get_dropout: null argument");
+    *seed = net->drop_seed;
+    *step = net->drop_step;
+    if (net->step_dev) {
+        SK_HIP(hipStreamSynchronize(net->last_stream));
+        SK_HIP(hipMemcpy(step, net->step_dev, sizeof(uint64_t), hipMemcpyDeviceToHost));
+    }
+    return SK_OK;
+}
+
 sk_status sknet_plan(sknet_t *net, int32_t n, int32_t h, int32_t w, int32_t pad, int32_t mode)
 {
     SK_TRY(check_net(net));
@@ -474,25 +693,27 @@ sk_status sknet_plan(sknet_t *net, int32_t n, int32_t h, int32_t w, int32_t pad,
     const int training = mode == 1 || mode == 3;
     std::vector<Dims> dims;
     int pt = 0, pl = 0;
-    SK_TRY(infer(net, h, w, pad, dims, &pt, &pl));
-    const int L = (int)net->layers.size();
+    std::vector<sk_layer> layers;                  // those that the plan will run
+    for (const auto &l : net->all_layers)
+        if (training || l.kind != SK_DROPOUT) layers.push_back(l);
+    SK_TRY(infer(net, layers, h, w, pad, dims, &pt, &pl));
+    const int L = (int)layers.size();
     if (training)
         for (int i = 0; i < L; ++i)
-            if (net->layers[i].kind == SK_MAXPOOL && net->layers[i].s != 1)
+            if (layers[i].kind == SK_MAXPOOL && layers[i].s != 1)
                 return fail(SK_EUNSUPPORTED, "plan: training through a down-sampling pool is not built");
     if (training && net->dtype != SK_F32)
         for (int i = 0; i < L; ++i)
-            if (net->layers[i].kind == SK_CONV && net->layers[i].k > 4)
-                return fail(SK_EUNSUPPORTED, "plan: the 16-bit kernels for k > 4 (layer %d: %dx%d) are forward only; train in fp32", i, net->layers[i].k, net->layers[i].k);
+            if (layers[i].kind == SK_CONV && layers[i].k > 4)
+                return fail(SK_EUNSUPPORTED, "plan: the 16-bit kernels for k > 4 (layer %d: %dx%d) are forward only; train in fp32", i, layers[i].k, layers[i].k);
     if (training && net->dtype != SK_F32)
         for (int i = 1; i < L; ++i)      // data gradients: the GEMM's output maps are the layer's input maps (the first layer needs none)
-            if (net->layers[i].kind == SK_CONV && !sk::conv_h_supported(net->layers[i].k, net->layers[i].d, dims[i].c))
+            if (layers[i].kind == SK_CONV && !sk::conv_h_supported(layers[i].k, layers[i].d, dims[i].c))
                 return fail(SK_EUNSUPPORTED, "plan: the 16-bit data gradient of layer %d (%dx%d, d = %d, %d input maps) does not fit the LDS tile",
-                            i, net->layers[i].k, net->layers[i].k, net->layers[i].d, dims[i].c);
-    // keep the host masters (a planned net's masters may have been updated on the device)
-    if (net->planned)
-        for (int i = 0; i < (int)net->convs.size(); ++i) SK_TRY(sknet_get_weights(net, i, nullptr, nullptr));
+                            i, layers[i].k, layers[i].k, layers[i].d, dims[i].c);
+    if (net->planned) SK_TRY(save_state(net));
     net->release_plan();
+    net->activate(training);
     SK_HIP(hipGetDevice(&net->device));
     net->n = n; net->h = h; net->w = w; net->pad = pad ? 1 : 0; net->training = training ? 1 : 0;
     net->pad_top = pt; net->pad_left = pl;
@@ -514,8 +735,8 @@ sk_status sknet_plan(sknet_t *net, int32_t n, int32_t h, int32_t w, int32_t pad,
         if (!shape_ok || !half || !sk::head_train_supported(net->dtype, dims[L - 2].c, net->layers[L - 2].c_out, net->layers[L - 1].c_out))
             return fail(SK_EUNSUPPORTED, "plan: mode 3 needs 16-bit storage and a net that ends in 1x1 conv + ReLU, 1x1 conv with at most 48 input maps, "
                                          "208 hidden maps and 4 classes");
-        if (L >= 3 && net->layers[L - 3].kind == SK_CONV && net->layers[L - 3].relu)
-            return fail(SK_EUNSUPPORTED, "plan: mode 3 needs a pool (or a convolution without ReLU) in front of the head");
+        if (net->relu_behind(L - 3))
+            return fail(SK_EUNSUPPORTED, "plan: mode 3 needs a pool (or a layer without ReLU) in front of the head");
         net->fuse_head = true;
     }
     net->vpool.assign(L, 0);
@@ -612,6 +833,17 @@ sk_status sknet_plan(sknet_t *net, int32_t n, int32_t h, int32_t w, int32_t pad,
             if (s > scratch) scratch = s;
         }
     }
+    for (int i = 0; i < L && st == SK_OK; ++i) {
+        if (net->norm_of_layer[i] < 0) continue;
+        st = alloc_norm(net->norms[net->norm_of_layer[i]], training != 0, (long)n * dims[i].h * dims[i].w);
+        sk::NormSpan span{};
+        maps_span(net, dims[i], &span);
+        scratch = std::max(scratch, sk::norm_bwd_scratch_floats(span));
+    }
+    if (st == SK_OK && training && std::any_of(layers.begin(), layers.end(), [](const sk_layer &l) { return l.kind == SK_DROPOUT; })) {
+        hipError_t e = hipMalloc(reinterpret_cast<void **>(&net->step_dev), sizeof(uint64_t));
+        st = e == hipSuccess ? put_step(net) : fail(SK_ENOMEM, "plan: hipMalloc of the dropout counter failed: %s", hipGetErrorString(e));
+    }
     if (training && net->fuse_head) scratch = std::max(scratch, sk::head_train_scratch_floats(dims[L - 2].c, net->layers[L - 2].c_out));
     if (st == SK_OK && net->fuse_head) {
         ConvParams &c1 = net->convs[net->conv_of_layer[L - 2]];
@@ -646,6 +878,7 @@ sk_status sknet_plan(sknet_t *net, int32_t n, int32_t h, int32_t w, int32_t pad,
                  [&](const int32_t *lab, float *loss) { return sknet_backward(net, lab, loss, nullptr); });
     net->forward_done = net->backward_done = false;
     net->last_image = nullptr; net->last_prob = nullptr;
+    if (st == SK_OK) st = put_step(net);           // the warm-up pass does not count
     if (st != SK_OK) {
         std::string keep = g_last_error;
         net->release_plan();
@@ -664,6 +897,7 @@ sk_status sknet_forward(sknet_t *net, const float *image_dev, float *prob_dev, v
     net->last_image = image_dev;
     net->last_prob = prob_dev;
     net->backward_done = false;
+    if (net->step_dev) SK_HIP(sk::launch_step_add(net->step_dev, stream));      // a mask of its own for every pass
     for (int s = 0; s < (int)net->steps.size(); ++s) SK_TRY(run_forward_step(net, s, stream));
     net->forward_done = true;
     return SK_OK;
@@ -681,7 +915,36 @@ static sk_status backward_layer(sknet_t *net, int li, float *gcur, float *gnext,
     const Dims &in = net->dims[li], &out = net->dims[li + 1];
     // ReLU of the layer below acts on this layer's input: fuse its mask into whatever
     // kernel produces the gradient of that input
-    const float *relu_src = (li > 0 && net->layers[li - 1].kind == SK_CONV && net->layers[li - 1].relu) ? net->act[li] : nullptr;
+    float *relu_src = net->relu_behind(li - 1) ? net->act[li] : nullptr;
+    if (l.kind == SK_LAYERNORM) {
+        const NormParams &m = net->norms[net->norm_of_layer[li]];
+        sk::NormBwdArgs a{};
+        maps_span(net, in, &a);
+        a.dy = maps_view(net, gcur, out);
+        a.s = maps_view(net, net->act[li], in);
+        if (li > 0 && (parts & 2)) a.dx = maps_view(net, gnext, in);
+        a.mean = m.mean; a.rstd = m.rstd; a.gamma = m.gamma_dev;
+        if (parts & 1) {
+            a.dgamma = m.dgamma;
+            a.dbeta = m.dbeta;
+        }
+        a.scratch = wgrad_scratch;
+        a.scratch_floats = wgrad_cap ? wgrad_cap : sk::norm_bwd_scratch_floats(a);
+        a.relu_x = relu_src ? 1 : 0;
+        SK_HIP(sk::launch_layer_norm_bwd(a, stream));
+        return SK_OK;
+    }
+    if (l.kind == SK_DROPOUT) {
+        if (li == 0 || !(parts & 2)) return SK_OK;
+        sk::DropoutArgs a{};
+        maps_span(net, in, &a);
+        a.x = maps_view(net, gcur, out);
+        a.y = maps_view(net, gnext, in);
+        if (relu_src) a.relu_src = maps_view(net, relu_src, in);
+        a.drop = layer_mask(net, li);
+        SK_HIP(sk::launch_dropout(a, stream));
+        return SK_OK;
+    }
     if (l.kind == SK_CONV) {
         ConvParams &c = net->convs[net->conv_of_layer[li]];
         if (parts & 1) {
@@ -760,12 +1023,12 @@ static sk_status backward_impl(sknet_t *net, const int32_t *labels_dev, float *l
     } else {
         const float *logits = (half && net->layers[L - 1].kind != SK_CONV) ? net->logits_f32 : net->act[L];
         float *dz = half ? net->dz_f32 : gcur;
-        const bool masked = net->layers[L - 1].kind == SK_CONV && net->layers[L - 1].relu;
+        const bool masked = net->relu_behind(L - 1);
         // 16-bit nets: the loss kernel also writes the gradient in the octet layout the layers below read (when it can)
         const bool direct = half && !masked && sk::softmax_loss_writes_octets(o.c, o.h * o.w);
         SK_HIP(sk::launch_softmax_loss_f32(logits, labels_dev, dz, loss_dev, loss_partial, n, o.c, o.h * o.w, stream, direct ? gcur : nullptr,
                                            direct ? dt : 0));
-        if (masked) SK_HIP(sk::launch_relu_mask_f32(dz, net->act[L], o.count(n), stream));
+        if (masked) SK_HIP(sk::launch_relu_mask_f32(dz, logits, o.count(n), stream));
         if (half && !direct) SK_HIP(sk::launch_pad_pack_h(dz, gcur, dt, n, o.c, o.h, o.w, 0, 0, o.h, o.w, 0, stream));
     }
     for (int li = top; li >= 0; --li) {
@@ -815,6 +1078,13 @@ sk_status sknet_backward_noalloc(sknet_t *net, const int32_t *labels_dev, float 
                         "backward_noalloc: the %d x %d x %dx%d weight gradient needs %zu floats of scratch, the static buffer holds %zu "
                         "(use sknet_backward, whose scratch belongs to the plan)", c.c_out, c.c_in, c.k, c.k, need, cap);
     }
+    for (int i = 0; i < L; ++i) {
+        if (net->norm_of_layer[i] < 0) continue;
+        sk::NormSpan span{};
+        maps_span(net, net->dims[i], &span);
+        if (sk::norm_bwd_min_scratch_floats(span) > cap)
+            return fail(SK_EUNSUPPORTED, "backward_noalloc: the sums of a layer norm over %d maps do not fit the static buffer", net->dims[i].c);
+    }
     float *base = nullptr;
     SK_TRY(static_scratch(&base));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -828,10 +1098,10 @@ sk_status sknet_backward_noalloc(sknet_t *net, const int32_t *labels_dev, float 
 sk_status sknet_get_activation_grad(sknet_t *net, int32_t layer_idx, const int32_t *labels_dev, float *nchw_host)
 {
     SK_TRY(check_net(net));
-    const int L = (int)net->layers.size();
-    if (!nchw_host || !labels_dev || layer_idx < 0 || layer_idx >= L) return fail(SK_EINVAL, "get_activation_grad: bad arguments");
+    if (!nchw_host || !labels_dev || layer_idx < 0 || layer_idx >= (int)net->all_layers.size()) return fail(SK_EINVAL, "get_activation_grad: bad arguments");
     if (!net->planned || !net->training || !net->forward_done)
         return fail(SK_ESTATE, "get_activation_grad: needs a forward pass on a training plan");
+    const int L = (int)net->layers.size();
     hipStream_t stream = net->last_stream;
     float *loss = nullptr, *g = nullptr, *tmp = nullptr;
     SK_TRY(alloc_f(&loss, 1));
@@ -864,13 +1134,17 @@ sk_status sknet_sgd_step(sknet_t *net, float lr, float momentum, float weight_de
     net->last_stream = stream;
     // one launch updates every weight and bias tensor, a second rebuilds every packed form
     // (a net is a dozen small tensors: one launch each would cost more than the work)
-    const int nc = (int)net->convs.size();
+    const int nc = (int)net->convs.size() + (int)net->norms.size();
     const ConvParams *head = net->fuse_head ? &net->convs[net->conv_of_layer[(int)net->layers.size() - 2]] : nullptr;
     if (2 * nc > sk::BATCH_MAX) {
         for (auto &c : net->convs) {
             SK_HIP(sk::launch_sgd_f32(c.w_dev, c.dw, momentum != 0.f ? c.vw : nullptr, c.wcount(), lr, momentum, weight_decay, stream));
             SK_HIP(sk::launch_sgd_f32(c.b_dev, c.db, momentum != 0.f ? c.vb : nullptr, c.c_out, lr, momentum, weight_decay, stream));
             SK_TRY(repack_conv(c, true, net->dtype, stream));
+        }
+        for (auto &m : net->norms) {
+            SK_HIP(sk::launch_sgd_f32(m.gamma_dev, m.dgamma, momentum != 0.f ? m.vgamma : nullptr, m.c, lr, momentum, weight_decay, stream));
+            SK_HIP(sk::launch_sgd_f32(m.beta_dev, m.dbeta, momentum != 0.f ? m.vbeta : nullptr, m.c, lr, momentum, weight_decay, stream));
         }
         if (head) SK_HIP(sk::launch_pack_head_w1(head->w_dev, net->head_w1p, net->dtype, head->c_out, head->c_in, stream));
         return SK_OK;
@@ -889,6 +1163,10 @@ sk_status sknet_sgd_step(sknet_t *net, float lr, float momentum, float weight_de
             ph[np++] = {c.w_dev, c.wp16_fwd, c.c_out, c.c_in, c.k, 0, c.mt16};
             if (c.wp16_bwd) ph[np++] = {c.w_dev, c.wp16_bwd, c.c_out, c.c_in, c.k, 1, c.mt16_bwd};
         }
+    }
+    for (auto &m : net->norms) {
+        sb.w[sb.n] = m.gamma_dev; sb.dw[sb.n] = m.dgamma; sb.v[sb.n] = momentum != 0.f ? m.vgamma : nullptr; sb.count[sb.n] = m.c; ++sb.n;
+        sb.w[sb.n] = m.beta_dev; sb.dw[sb.n] = m.dbeta; sb.v[sb.n] = momentum != 0.f ? m.vbeta : nullptr; sb.count[sb.n] = m.c; ++sb.n;
     }
     if (head && np < sk::BATCH_MAX) {      // (16-bit storage) the fragments of a 1x1 layer in groups of one tile; the tiles behind its last stay zero
         ph[np++] = {head->w_dev, net->head_w1p, head->c_out, head->c_in, 1, 0, 1};
@@ -916,8 +1194,9 @@ sk_status sknet_get_grad(sknet_t *net, int32_t conv_idx, float *dw_host, float *
 sk_status sknet_get_activation(sknet_t *net, int32_t layer_idx, float *nchw_host)
 {
     SK_TRY(check_net(net));
-    if (!nchw_host || layer_idx < -1 || layer_idx >= (int)net->layers.size()) return fail(SK_EINVAL, "get_activation: bad arguments");
+    if (!nchw_host || layer_idx < -1 || layer_idx >= (int)net->all_layers.size()) return fail(SK_EINVAL, "get_activation: bad arguments");
     if (!net->forward_done) return fail(SK_ESTATE, "get_activation: no forward pass yet");
+    if (layer_idx >= 0) layer_idx = net->maps_of[layer_idx] - 1;      // (a dropout layer that an inference plan leaves out: the layer in front of it)
     if (layer_idx >= 0 && !net->kept(layer_idx))
         return fail(SK_ESTATE, "get_activation: this plan fuses layer %d with its neighbours; plan with mode 2 to keep every layer", layer_idx);
     SK_HIP(hipStreamSynchronize(net->last_stream));
@@ -1010,10 +1289,13 @@ sk_status sknet_step_name(const sknet_t *net, int32_t step, char *name, int32_t 
     else if (st.kind == 3) snprintf(name, cap, "head_fused");
     else {
         const sk_layer &l = net->layers[st.arg];
-        if (l.kind == SK_CONV)
-            snprintf(name, cap, "conv%d_k%d_d%d_o%d%s%s", st.arg, l.k, l.d, l.c_out, net->pending[st.arg] ? "_hpool" : "",
+        const int user = net->user_of[st.arg];
+        if (l.kind == SK_LAYERNORM) snprintf(name, cap, "norm%d", user);
+        else if (l.kind == SK_DROPOUT) snprintf(name, cap, "dropout%d", user);
+        else if (l.kind == SK_CONV)
+            snprintf(name, cap, "conv%d_k%d_d%d_o%d%s%s", user, l.k, l.d, l.c_out, net->pending[st.arg] ? "_hpool" : "",
                      st.arg == 0 && net->c1_pool ? "_pool" : net->vpool[st.arg] ? "_vpool" : "");
-        else snprintf(name, cap, "pool%d_k%d_d%d_s%d", st.arg, l.k, l.d, l.s);
+        else snprintf(name, cap, "pool%d_k%d_d%d_s%d", user, l.k, l.d, l.s);
     }
     return SK_OK;
 }
@@ -1046,10 +1328,10 @@ sk_status sknet_time_backward_step(sknet_t *net, const int32_t *labels_dev, int3
                                    float *avg_ms)
 {
     SK_TRY(check_net(net));
-    const int L = (int)net->layers.size();
-    if (!avg_ms || !labels_dev || iters < 1 || part < 0 || part > 2 || (part != 2 && (layer_idx < 0 || layer_idx >= L)))
+    if (!avg_ms || !labels_dev || iters < 1 || part < 0 || part > 2 || (part != 2 && (layer_idx < 0 || layer_idx >= (int)net->all_layers.size())))
         return fail(SK_EINVAL, "time_backward_step: bad arguments");
     if (!net->planned || !net->training || !net->forward_done) return fail(SK_ESTATE, "time_backward_step: needs a forward pass on a training plan");
+    const int L = (int)net->layers.size();
     if (part == 0 && net->layers[layer_idx].kind != SK_CONV) return fail(SK_EINVAL, "time_backward_step: layer %d has no weights", layer_idx);
     if (part == 1 && layer_idx == 0) return fail(SK_EINVAL, "time_backward_step: layer 0 has no input gradient");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);

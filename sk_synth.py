@@ -20,6 +20,15 @@ def pool(k, d=1, s=1):
     return {"type": "pool", "k": k, "d": d, "s": s}
 
 
+def norm(relu=False):
+    """Layer norm over the maps of each pixel."""
+    return {"type": "norm", "k": 1, "d": 1, "s": 1, "relu": relu}
+
+
+def dropout(p):
+    return {"type": "dropout", "k": 1, "d": 1, "s": 1, "p": p}
+
+
 def tiny_sknet_layers():
     """Config C1: conv 1->8 k4 d1, pool k2 d1, conv 8->16 k5 d2, pool k2 d2, 1x1 16->32, 1x1 32->2."""
     return [conv(8, 4, 1), pool(2, 1), conv(16, 5, 2), pool(2, 2), conv(32, 1, 1), conv(2, 1, 1, relu=False)]

@@ -158,3 +158,72 @@ def test_binding_refuses_what_is_no_gpu_tensor():
         for t in (torch.zeros(3, 4), np.zeros((3, 4), np.float32), None):
             with pytest.raises(TypeError):
                 call(t)
+
+
+# ---- the layers of a net
+
+def test_net_layers_shapes_and_refusals():
+    import sk_synth as S
+    layers = [S.conv(8, 4, 1, relu=False), S.norm(relu=True), S.pool(2, 1), S.conv(16, 5, 2), S.dropout(0.5), S.norm(), S.conv(2, 1, 1, relu=False)]
+    for dtype in ("f32", "bf16", "f16"):
+        net = B.SKNet(layers, 1, 2, dtype=dtype)
+        assert net.num_convs() == 3 and net.num_norms() == 2 and [net.norm_size(i) for i in range(2)] == [8, 16]
+        plain = B.SKNet([l for l in layers if l["type"] in ("conv", "pool")], 1, 2)
+        assert net.context() == plain.context()
+        shapes = net.infer_shapes(60, 50)
+        assert [s[1:] for i, s in enumerate(shapes) if i not in (2, 5, 6)] == [s[1:] for s in plain.infer_shapes(60, 50)]
+        g, b = net.get_norm(1)
+        assert (g == 1).all() and (b == 0).all()
+        net.set_norm(1, beta=np.arange(16))
+        net.set_norm(0, gamma=np.full(8, 2.0))
+        assert (net.get_norm(1)[0] == 1).all() and (net.get_norm(1)[1] == np.arange(16)).all() and (net.get_norm(0)[0] == 2).all()
+        assert net.get_dropout() == (0, 0)
+        net.set_dropout((1 << 64) - 1, 77)
+        assert net.get_dropout() == ((1 << 64) - 1, 77)
+        for bad in (lambda: net.set_norm(2), lambda: net.get_norm(-1), lambda: net.get_norm_grad(0), lambda: net.set_dropout(1, 1 << 40)):
+            with pytest.raises(B.SknetError):
+                bad()
+        with pytest.raises(ValueError):
+            net.set_norm(0, gamma=np.zeros(9))
+        net.close()
+    for layer in (B.SkLayer(B.SK_LAYERNORM, 0, 2, 1, 1, 0), B.SkLayer(B.SK_DROPOUT, 100, 1, 2, 1, 0), B.SkLayer(B.SK_LAYERNORM, 0, 1, 1, 2, 0),
+                  B.SkLayer(B.SK_DROPOUT, 65537, 1, 1, 1, 0), B.SkLayer(B.SK_DROPOUT, -1, 1, 1, 1, 0), B.SkLayer(B.SK_DROPOUT, 5, 1, 1, 1, 1), B.SkLayer(4, 0, 1, 1, 1, 0)):
+        arr, out = (B.SkLayer * 2)(B.SkLayer(B.SK_CONV, 2, 1, 1, 1, 0), layer), C.c_void_p()
+        assert B.STATUS_NAMES[B.lib.sknet_create(arr, 2, 1, 2, 0, 0, C.byref(out))] in ("SK_EINVAL", "SK_ESHAPE") and not out.value
+        assert B.STATUS_NAMES[B.lib.sknet3d_create(arr, 2, 1, 2, C.byref(out))] in ("SK_EINVAL", "SK_ESHAPE")
+    for kind in (B.SK_LAYERNORM, B.SK_DROPOUT):            # 2-D nets only
+        arr, out = (B.SkLayer * 2)(B.SkLayer(B.SK_CONV, 2, 1, 1, 1, 0), B.SkLayer(kind, 0, 1, 1, 1, 0)), C.c_void_p()
+        assert B.STATUS_NAMES[B.lib.sknet3d_create(arr, 2, 1, 2, C.byref(out))] == "SK_EINVAL"
+    with pytest.raises(B.SknetError):
+        B.SKNet([S.dropout(0.5)], 2, 2)
+    with pytest.raises(ValueError):
+        B.SKNet([S.conv(2, 1), S.dropout(1.5)], 1, 2)
+
+
+def test_oracle_net_gradients_by_differences():
+    import sk_synth as S
+    from oracle import nets as NETS
+    layers = [S.conv(5, 2, 1, relu=False), S.norm(relu=True), S.dropout(0.3), S.pool(2, 1), S.norm(), S.conv(6, 1), S.dropout(0.5), S.conv(3, 1, relu=False)]
+    ws, bs = S.he_normal_weights(layers, 2, 7, bias_scale=0.1)
+    ws, bs = [w.astype(np.float64) for w in ws], [b.astype(np.float64) for b in bs]
+    rng = np.random.default_rng(8)
+    norms = [(1 + 0.3 * rng.normal(size=5), 0.3 * rng.normal(size=5)), (1 + 0.3 * rng.normal(size=5), 0.3 * rng.normal(size=5))]
+    img, lab = rng.random((1, 2, 6, 5)), rng.integers(0, 3, (1, 6, 5)).astype(np.int32)
+    drop = (99, 4)
+
+    def loss():
+        _, acts, am = NETS.sknet_forward(img, layers, ws, bs, keep=True, norms=norms, drop=drop)
+        return acts, am, NETS.L.softmax_loss(acts[-1], lab)[0]
+
+    acts, am, _ = loss()
+    grads = []
+    _, dws, dbs, _ = NETS.sknet_backward(layers, ws, acts, am, lab, norms=norms, drop=drop, norm_grads=grads)
+    for arr, grad in [(ws[0], dws[0]), (ws[1], dws[1]), (bs[0], dbs[0])] + [(norms[i][j], grads[i][j]) for i in range(2) for j in range(2)]:
+        for i in list(np.ndindex(arr.shape))[::3]:
+            old = arr[i]
+            arr[i] = old + 1e-5
+            up = loss()[2]
+            arr[i] = old - 1e-5
+            down = loss()[2]
+            arr[i] = old
+            assert abs((up - down) / 2e-5 - grad[i]) <= 1e-6
