@@ -276,6 +276,14 @@ def _orders(shape, strides, axis):
     return found
 
 
+@functools.lru_cache(maxsize=4096)
+def _workspace(dtype, layout, n, c, plane):
+    """Bytes of a backward call's workspace: a matter of the extent alone."""
+    need = C.c_uint64()
+    _check(lib.sknet_layer_norm_workspace(C.byref(SkExtent(dtype, layout, n, c, plane)), C.byref(need)))
+    return need.value
+
+
 class _Operator:
     """One call of an operator: its stream and device, and its tensors as views of one extent."""
 
@@ -286,18 +294,20 @@ class _Operator:
             raise ValueError("%s has no axis %d" % (what, axis))
         self.x, self.what, self.axis, self.device = x, what, axis % x.dim(), x.device
         self.views = {}
-        current = torch.cuda.current_stream(x.device)
         self.scope = None
-        if stream is not None and not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device=x.device)
+        elsewhere = self.device.index != torch.cuda.current_device()
+        if stream is None and not elsewhere:       # the usual call: a stream object would take 2 us
+            self.stream = torch._C._cuda_getCurrentRawStream(self.device.index)
+            return
         if stream is None:
-            stream = current
-        elif stream.device != x.device:
+            stream = torch.cuda.current_stream(x.device)
+        elif not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=x.device)
+        if stream.device != x.device:
             raise ValueError("the stream is not one of %s" % (x.device,))
         # the call runs, and what it allocates belongs, there
-        if stream.cuda_stream != current.cuda_stream or x.device.index != torch.cuda.current_device():
-            self.scope = torch.cuda.stream(stream)
-        self.stream = C.c_void_p(stream.cuda_stream)
+        self.scope = torch.cuda.stream(stream)
+        self.stream = stream.cuda_stream
 
     def __enter__(self):
         if self.scope is not None:
@@ -413,9 +423,7 @@ def layer_norm_backward(dy, s, mean, rstd, gamma=None, axis=-1, dsum=None, p=0.0
         if parameters:
             dgamma = torch.empty(c, dtype=torch.float32, device=dy.device) if dgamma is None else dgamma
             dbeta = torch.empty(c, dtype=torch.float32, device=dy.device) if dbeta is None else dbeta
-            need = C.c_uint64()
-            _check(lib.sknet_layer_norm_workspace(C.byref(op.extent), C.byref(need)))
-            bytes_ = need.value
+            bytes_ = _workspace(op.extent.dtype, *op.order)
             if bytes_:
                 workspace = torch.empty(bytes_, dtype=torch.uint8, device=dy.device)
         elif dgamma is not None or dbeta is not None:

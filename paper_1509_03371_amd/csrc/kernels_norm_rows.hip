@@ -301,16 +301,20 @@ __device__ __forceinline__ void put_values(float *out, int c, int c0, const floa
     }
 }
 
-// Backwards: a workgroup walks rows gridDim.x * T / G apart and keeps its lanes' sums for dgamma and dbeta in registers until the end, where they
-// go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta themselves if there is one workgroup.
+// Backwards: a workgroup takes R = T / G rows at a time, gridDim.x * R apart, and keeps its lanes' sums for dgamma and dbeta in registers until the end,
+// where they are added up over the R rows' lanes through LDS and go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta
+// themselves if there is one workgroup.  Eight waves a workgroup, not four or less: half the copies, whose writing and adding up cost 25 of 171 us for
+// 16384 x 4096 bf16.
 template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T, 4) void norm_rows_bwd_kernel(NormBwdArgs a)
 {
-    constexpr int W = T / 64;
+    constexpr int W = T / 64, R = T / G;
+    constexpr int each = G < 64 ? 1 : G / 64;           // waves that hold one row's channels
     __shared__ float part[G > 64 ? 4 * W : 1];
-    __shared__ float sums[G < T ? W : 1][G < T ? G * K * 8 + 1 : 1];
+    __shared__ float sums[R > 1 ? W / each : 1][R > 1 ? G * K * 8 + 1 : 1];
     const Row<DT, G> r(a.c);
     const bool exact = a.c == 8 * G * K;
     const uint64_t counter = ADD ? a.drop.base() : 0;
+    const int wave = uniform(threadIdx.x >> 6), group = wave / each;
     float gamma[K][8], dg[K][8], db[K][8];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -326,31 +330,35 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
         }
     }
     int half = 0;
-    for (long row0 = first_row<G, T>(); row0 < a.n; row0 += row_step<G, T>()) {     // (G > 64: every thread alike)
-        const long row = row0 + r.sub;
-        if (G < 64 && row >= a.n) break;
+    for (long first = blockIdx.x * (long)R; first < a.n; first += gridDim.x * (long)R) {     // (every thread alike)
+        const long row0 = first + (G < 64 ? wave * (64 / G) : group);
+        const bool mine = row0 + r.sub < a.n;
+        if (G <= 64 && !mine) continue;                 // (G > 64: all come to the barrier)
         Words<DT, 8> vy[K], vs[K], vd[ADD ? K : 1];
+        float mean = 0.f, rstd = 0.f, sg = 0.f, sgh = 0.f;
+        if (mine) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            r.load(r.from(a.dy, row0), r.offset(a.dy), k, vy[k]);
-            r.load(r.from(a.s, row0), r.offset(a.s), k, vs[k]);
-        }
-        if (ADD && a.dsum.p)
+            for (int k = 0; k < K; ++k) {
+                r.load(r.from(a.dy, row0), r.offset(a.dy), k, vy[k]);
+                r.load(r.from(a.s, row0), r.offset(a.s), k, vs[k]);
+            }
+            if (ADD && a.dsum.p)
 #pragma unroll
-            for (int k = 0; k < K; ++k) r.load(r.from(a.dsum, row0), r.offset(a.dsum), k, vd[ADD ? k : 0]);
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float sg = 0.f, sgh = 0.f;
+                for (int k = 0; k < K; ++k) r.load(r.from(a.dsum, row0), r.offset(a.dsum), k, vd[ADD ? k : 0]);
+            mean = a.mean[row0 + r.sub];
+            rstd = a.rstd[row0 + r.sub];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            r.fit(k, exact, vy[k]);                     // behind the last channel dy is zero
-            r.fit(k, exact, vs[k]);
+            for (int k = 0; k < K; ++k) {
+                r.fit(k, exact, vy[k]);                 // behind the last channel dy is zero
+                r.fit(k, exact, vs[k]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float h = (vs[k][j] - mean) * rstd, y = vy[k][j], g = y * gamma[k][j];
-                sg += g;
-                sgh += g * h;
-                dg[k][j] += y * h;
-                db[k][j] += y;
+                for (int j = 0; j < 8; ++j) {
+                    const float h = (vs[k][j] - mean) * rstd, y = vy[k][j], g = y * gamma[k][j];
+                    sg += g;
+                    sgh += g * h;
+                    dg[k][j] += y * h;
+                    db[k][j] += y;
+                }
             }
         }
         sg = sum_lanes<(G < 64 ? G : 64)>(sg);
@@ -359,18 +367,18 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
             float *p = part + half * 2 * W;             // two halves in turn: one barrier a row
             half ^= 1;
             if ((threadIdx.x & 63) == 0) {
-                p[threadIdx.x >> 6] = sg;
-                p[W + (threadIdx.x >> 6)] = sgh;
+                p[wave] = sg;
+                p[W + wave] = sgh;
             }
             __syncthreads();
             sg = sgh = 0.f;
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                sg += p[i];
-                sgh += p[W + i];
+            for (int i = 0; i < each; ++i) {
+                sg += p[group * each + i];
+                sgh += p[W + group * each + i];
             }
         }
-        if (!a.dx.p && (!ADD || !a.dresidual.p)) continue;
+        if (!mine || (!a.dx.p && (!ADD || !a.dresidual.p))) continue;
         const float mg = sg / (float)a.c, mgh = sgh / (float)a.c;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -386,13 +394,13 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
     const long cp = norm_copy_floats(a.c) / 2;
     auto put = [&](const float (&acc)[K][8], float *own, int which) {
         float *out = alone ? own : a.scratch + (blockIdx.x * 2L + which) * cp;
-        if (G == T) {                                   // every channel belongs to one lane of the workgroup
+        if (R == 1) {                                   // every channel belongs to one lane of the workgroup
             if (out)
 #pragma unroll
                 for (int k = 0; k < K; ++k) put_values(out, a.c, r.channel(k), acc[k]);
             return;
         }
-        // rows of one wave first, then the waves in order
+        // rows of one wave first, then the groups in order
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -400,14 +408,14 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
                 float v = acc[k][j];
 #pragma unroll
                 for (int i = G; i < 64; i *= 2) v += __shfl_xor(v, i);
-                if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][8 * (k * G + r.lane) + j] = v;
+                if (G >= 64 || (threadIdx.x & 63) < G) sums[group][r.channel(k) + j] = v;
             }
         __syncthreads();
         if (out)
             for (int c = threadIdx.x; c < a.c; c += T) {
                 float v = 0.f;
 #pragma unroll
-                for (int i = 0; i < W; ++i) v += sums[i][c];
+                for (int i = 0; i < W / each; ++i) v += sums[i][c];
                 out[c] = v;
             }
         __syncthreads();
@@ -507,14 +515,14 @@ template <class F> void pick_rows(int c, bool far, F f)
 // the same backwards, where a lane also holds gamma and two sums a channel
 template <class F> void pick_rows_bwd(int c, bool far, F f)
 {
-    if (c <= 8 && !far) return f(num<1>{}, num<1>{}, num<256>{});
-    if (c <= 64 && !far) return f(num<8>{}, num<1>{}, num<256>{});
-    if (c <= 128 && !far) return f(num<16>{}, num<1>{}, num<256>{});
-    if (c <= 256 && !far) return f(num<32>{}, num<1>{}, num<256>{});
-    if (c <= 512) return f(num<64>{}, num<1>{}, num<256>{});
-    if (c <= 1024) return f(num<64>{}, num<2>{}, num<256>{});
-    if (c <= 2048) return f(num<128>{}, num<2>{}, num<128>{});
-    if (c <= 4096) return f(num<256>{}, num<2>{}, num<256>{});
+    if (c <= 8 && !far) return f(num<1>{}, num<1>{}, num<512>{});
+    if (c <= 64 && !far) return f(num<8>{}, num<1>{}, num<512>{});
+    if (c <= 128 && !far) return f(num<16>{}, num<1>{}, num<512>{});
+    if (c <= 256 && !far) return f(num<32>{}, num<1>{}, num<512>{});
+    if (c <= 512) return f(num<64>{}, num<1>{}, num<512>{});
+    if (c <= 1024) return f(num<64>{}, num<2>{}, num<512>{});
+    if (c <= 2048) return f(num<128>{}, num<2>{}, num<512>{});
+    if (c <= 4096) return f(num<256>{}, num<2>{}, num<512>{});
     if (c <= 8192) return f(num<512>{}, num<2>{}, num<512>{});
     return f(num<1024>{}, num<2>{}, num<1024>{});
 }
