@@ -212,8 +212,10 @@ template <int DT, int LAYOUT, int V> __global__ __launch_bounds__(64) void norm_
         for (int j = 0; j < 8; ++j) {
             const float g = sum_lanes<64>(dg[j]), s = sum_lanes<64>(db[j]);
             if (t.lane == 0 && 8 * o + j < a.c) {
-                a.scratch[blockIdx.y * 2L * cp + 8 * o + j] = g;
-                a.scratch[(blockIdx.y * 2L + 1) * cp + 8 * o + j] = s;
+                float *dgamma = gridDim.y == 1 ? a.dgamma : a.scratch + blockIdx.y * 2L * cp;
+                float *dbeta = gridDim.y == 1 ? a.dbeta : a.scratch + (blockIdx.y * 2L + 1) * cp;
+                if (dgamma) dgamma[8 * o + j] = g;
+                if (dbeta) dbeta[8 * o + j] = s;
             }
         }
     }
@@ -254,7 +256,7 @@ hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t 
                 const long row = tiles_of_image(a, 64 * v()), tiles = a.n * row;
                 const int shares = (int)std::min<long>(std::min(copies, 16), tiles);
                 norm_deep_planes_wgrad_kernel<dt(), layout(), v()><<<dim3(std::min((a.c + 7) / 8, 65536), shares), 64, 0, stream>>>(a, tiles, row);
-                (void)launch_norm_reduce(a.scratch, shares, a.dgamma, a.dbeta, a.c, stream);
+                if (shares > 1) (void)launch_norm_reduce(a.scratch, shares, a.dgamma, a.dbeta, a.c, stream);
             }
             if (!a.dx.p && !a.dresidual.p) return;
             const long row = tiles_of_image(a, p() * v()), tiles = a.n * row;

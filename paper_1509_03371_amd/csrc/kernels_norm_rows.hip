@@ -487,8 +487,10 @@ template <int DT> __global__ __launch_bounds__(1024) void norm_long_rows_wgrad_k
                 db[j] += vy[j];
             }
         }
-        put_values(a.scratch + blockIdx.y * 2L * cp, a.c, r.channel(k), dg);
-        put_values(a.scratch + (blockIdx.y * 2L + 1) * cp, a.c, r.channel(k), db);
+        float *dgamma = gridDim.y == 1 ? a.dgamma : a.scratch + blockIdx.y * 2L * cp;
+        float *dbeta = gridDim.y == 1 ? a.dbeta : a.scratch + (blockIdx.y * 2L + 1) * cp;
+        if (dgamma) put_values(dgamma, a.c, r.channel(k), dg);
+        if (dbeta) put_values(dbeta, a.c, r.channel(k), db);
     }
 }
 
@@ -599,12 +601,19 @@ hipError_t launch_norm_rows(const NormArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
+// Rounds of rows that one workgroup takes alone, which then writes the sums themselves: no second launch, no workspace.  Alone and shared out, us: two rounds
+// (16 rows of 777 channels) 7.3 and 8.2, 4 x 4096 7.6 and 8.5; three (24 x 777) 8.5 and 8.2, five (37 x 777) 10.9 and 8.2.
+constexpr long kAloneRounds = 2;
+
 // (rows far apart take as many: their workgroups hold no more of them)
 int norm_rows_bwd_copies(const NormSpan &s)
 {
     if (s.c > kLongRowBwd) return (int)std::min<long>(s.n, 16);
     int copies = 1;
-    pick_rows_bwd(s.c, false, [&](auto g, auto, auto t) { copies = (int)std::min<long>((s.n + t() / g() - 1) / (t() / g()), 256 * 1024 / t()); });
+    pick_rows_bwd(s.c, false, [&](auto g, auto, auto t) {
+        const long rounds = (s.n + t() / g() - 1) / (t() / g());
+        copies = rounds <= kAloneRounds ? 1 : (int)std::min<long>(rounds, 256 * 1024 / t());
+    });
     return copies;
 }
 
@@ -616,8 +625,8 @@ hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t st
     pick_type(a.dtype, [&](auto dt) {
         if (a.c > kLongRowBwd) {
             if (sums) {
-                norm_long_rows_wgrad_kernel<dt()><<<dim3((unsigned)std::min((a.c + 8191) / 8192, 65536), std::min(copies, 16)), 1024, 0, stream>>>(a);
-                (void)launch_norm_reduce(a.scratch, std::min(copies, 16), a.dgamma, a.dbeta, a.c, stream);
+                norm_long_rows_wgrad_kernel<dt()><<<dim3((unsigned)std::min((a.c + 8191) / 8192, 65536), copies), 1024, 0, stream>>>(a);
+                if (copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
             }
             if (a.dx.p || a.dresidual.p) norm_long_rows_bwd_kernel<dt()><<<norm_blocks(a.n, 1), 1024, 0, stream>>>(a);
             return;

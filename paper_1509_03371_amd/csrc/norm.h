@@ -51,8 +51,7 @@ struct NormBwdArgs : NormSpan {
     int relu_x;
     DropMask drop;
 };
-size_t norm_bwd_scratch_floats(const NormSpan &s);        // of the fastest launch
-size_t norm_bwd_min_scratch_floats(const NormSpan &s);    // below this the launch is refused (hipErrorInvalidValue)
+size_t norm_bwd_scratch_floats(const NormSpan &s);        // of the fastest launch; with less, fewer workgroups share the sums out
 hipError_t launch_layer_norm_bwd(const NormBwdArgs &a, hipStream_t stream);
 
 // *step += 1: one more forward pass (a kernel, so that a recorded pass moves on at every replay)

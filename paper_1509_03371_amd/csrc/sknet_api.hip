@@ -1078,13 +1078,6 @@ sk_status sknet_backward_noalloc(sknet_t *net, const int32_t *labels_dev, float 
                         "backward_noalloc: the %d x %d x %dx%d weight gradient needs %zu floats of scratch, the static buffer holds %zu "
                         "(use sknet_backward, whose scratch belongs to the plan)", c.c_out, c.c_in, c.k, c.k, need, cap);
     }
-    for (int i = 0; i < L; ++i) {
-        if (net->norm_of_layer[i] < 0) continue;
-        sk::NormSpan span{};
-        maps_span(net, net->dims[i], &span);
-        if (sk::norm_bwd_min_scratch_floats(span) > cap)
-            return fail(SK_EUNSUPPORTED, "backward_noalloc: the sums of a layer norm over %d maps do not fit the static buffer", net->dims[i].c);
-    }
     float *base = nullptr;
     SK_TRY(static_scratch(&base));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
