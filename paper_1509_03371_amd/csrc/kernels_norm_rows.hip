@@ -10,6 +10,7 @@ namespace {
 template <int DT, int G> struct Row {
     typedef elem_t<DT> E;
     static constexpr int S = sizeof(E);
+    static constexpr bool SHORT = G == 1 || G == 64;    // may have rows of fewer than eight (64: rows too far apart for other G)
     const int c;
     const int lane, sub;                                // of the row's G; row among the wave's
 
@@ -20,14 +21,15 @@ template <int DT, int G> struct Row {
     template <int D> __device__ __forceinline__ void load(src_t p, uint32_t off, int k, Words<D, 8> &w) const
     {
         constexpr int size = sizeof(elem_t<D>);
-        if constexpr (G == 1) {                         // lines of up to eight elements
+        if (SHORT && c < 8) {                           // lines of fewer than eight elements, one by one
             w.clear();
+            if (channel(k) == 0)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < c) {
-                    if constexpr (D == 0) w.w[j] = *reinterpret_cast<const uint32_t *>(p + off + 4 * j);
-                    else w.w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p + off + 2 * j) << 16 * (j & 1);
-                }
+                for (int j = 0; j < 7; ++j)
+                    if (j < c) {
+                        if constexpr (D == 0) w.w[j] = *reinterpret_cast<const uint32_t *>(p + off + 4 * j);
+                        else w.w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p + off + 2 * j) << 16 * (j & 1);
+                    }
         } else {
             w.load(p, off + size * std::min(channel(k), c - 8));
         }
@@ -36,7 +38,7 @@ template <int DT, int G> struct Row {
     template <int D> __device__ __forceinline__ void fit(int k, bool exact, Words<D, 8> &w) const
     {
         constexpr int n = Words<D, 8>::count;
-        if (G == 1 || exact) return;
+        if (exact || (SHORT && c < 8)) return;
         const int left = c - channel(k);
         if (c % 8) {                                    // down by 8 - c % 8 elements in the one lane that read over the end
             const bool tail = left > 0 && left < 8;

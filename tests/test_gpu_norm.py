@@ -299,7 +299,7 @@ def test_a_block_of_a_network_by_differences():
             assert abs(slope - mine) <= 1e-4 * np.sqrt((to64(grad) ** 2).sum() * (d ** 2).sum()), (shape, i)
 
 
-@pytest.mark.parametrize("shape,stride", [((70, 40), 1 << 24), ((3, 600), 1 << 31), ((2, 30, 9), 1 << 27), ((1, 9, 70), 1 << 29), ((1, 5, 2), 1 << 29)], ids=str)
+@pytest.mark.parametrize("shape,stride", [((70, 40), 1 << 24), ((70, 5), 1 << 24), ((67, 1), 1 << 24), ((65, 8), 1 << 24), ((3, 600), 1 << 31), ((2, 30, 9), 1 << 27), ((1, 9, 70), 1 << 29), ((1, 5, 2), 1 << 29)], ids=str)
 def test_strides_that_32_bits_do_not_span(shape, stride):
     from paper_1509_03371_amd import binding as B
     size = stride * (shape[0] if len(shape) == 2 else shape[0] * shape[1])
@@ -330,3 +330,55 @@ def test_strides_that_32_bits_do_not_span(shape, stride):
         close(g, to64(w), 2.0 ** -6 * np.abs(to64(w)) + 1e-3, "backward")
     out = far(torch.zeros_like(x), 32768)
     assert np.array_equal(to64(B.dropout(fx, 0.4, 9, axis=1, out=out)), to64(B.dropout(x, 0.4, 9, axis=1)))
+
+
+@pytest.mark.parametrize("shape", [((1 << 21) + 3, 1100), (2, 9, (1 << 27) + 5), (3, 17, (1 << 26) + 1)], ids=str)
+def test_tensors_of_more_than_32_bits_of_elements(shape):
+    from paper_1509_03371_amd import binding as B
+    x = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+    last = 300
+    tail = x[-last:] if len(shape) == 2 else x[-1:, :, -last:]
+    tail.copy_(torch.randn(tail.shape, device="cuda"))
+    c = shape[1]
+    positions = np.arange(x.numel() // c - last, x.numel() // c, dtype=np.uint64)
+    keep = ON.keep_mask(positions, c, 0.25, 5, 6)
+    part = to64(tail) if len(shape) == 2 else to64(tail)[0].T
+    y = B.dropout(x, 0.25, 5, 6, axis=1)
+    got = to64(y[-last:]) if len(shape) == 2 else to64(y[-1, :, -last:]).T
+    ref = np.where(keep, part * (65536.0 / (65536 - ON.threshold(0.25))), 0.0)
+    close(got, ref, rounded(ref, "bf16", 2 * U * np.abs(ref)), "dropout")
+    out, s, mean, rstd = B.layer_norm(x, axis=1, p=0.25, seed=5, offset=6, out=y)
+    got = to64(out[-last:]) if len(shape) == 2 else to64(out[-1, :, -last:]).T
+    ry, rm, rr, by, bm, brs = norm_bounds(ref, 2 * U * np.abs(ref), None, None, 1e-5, "bf16")
+    close(got, ry, by, "y")
+    close(to64(mean).reshape(-1)[-last:], rm, bm, "mean")
+    assert (out[:5] == 0).all() if len(shape) == 2 else (out[0, :, :1000] == 0).all()
+    dx, _, dg, db = B.layer_norm_backward(x, s, mean, rstd, axis=1, dx=out)
+    t, rg, rb, et, eg, eb = bwd_bounds(part, to64(s[-last:]) if len(shape) == 2 else to64(s[-1, :, -last:]).T, to64(mean).reshape(-1)[-last:],
+                                       to64(rstd).reshape(-1)[-last:], None, None, "bf16")
+    got = to64(dx[-last:]) if len(shape) == 2 else to64(dx[-1, :, -last:]).T
+    close(got, t, rounded(t, "bf16", et), "dx")
+    # (zeros elsewhere add nothing to the sums, and no rounding)
+    close(dg, rg, eg, "dgamma")
+    close(db, rb, eb, "dbeta")
+
+
+@pytest.mark.parametrize("shape", [(5000, 20, 2), (700, 3, 3), (6, 2100, 3), (2, 2100, 70), (1, 40000, 5)], ids=str)
+def test_small_planes_and_many_channels(shape):
+    from paper_1509_03371_amd import binding as B
+    x, r, gamma, beta, dy, dsum = inputs(shape, "f32", 5)
+    x, r, dy, dsum = (place(a, "f32") for a in (x, r, dy, dsum))
+    gd, bd = torch.from_numpy(gamma).cuda(), torch.from_numpy(beta).cuda()
+    kw = dict(axis=1, p=0.3, seed=2, offset=1)
+    y, s, mean, rstd = B.layer_norm(x, gd, bd, residual=r, **kw)
+    dropped = ON.dropout(to64(x), 0.3, 2, 1)
+    rs = to64(r) + dropped
+    es = U * (2 * np.abs(dropped) + np.abs(rs)) * (1 + 4 * U)
+    ry, rm, rr, by, bm, brs = norm_bounds(rs, es, gamma, beta, 1e-5, "f32")
+    close(y, ry, by, "y")
+    close(rstd, rr, brs, "rstd")
+    dx, dres, dg, db = B.layer_norm_backward(dy, s, mean, rstd, gd, dsum=dsum, **kw)
+    t, rg, rb, et, eg, eb = bwd_bounds(to64(dy), to64(s), to64(mean), to64(rstd), gamma, to64(dsum), "f32")
+    close(dres, t, rounded(t, "f32", et), "dresidual")
+    close(dg, rg, eg, "dgamma")
+    close(db, rb, eb, "dbeta")
