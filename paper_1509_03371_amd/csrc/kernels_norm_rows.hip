@@ -269,12 +269,11 @@ __device__ __forceinline__ void put_gradients(const Row<DT, G> &r, const NormBwd
                                               const Words<DT, 8> &vs, const Words<DT, 8> &vd, const float (&gamma)[8], float mean, float rstd, float mg,
                                               float mgh)
 {
+    // rstd (gamma dy - mg - h mgh) with h = (s - mean) rstd, as (gamma dy) rstd - mg rstd - (s - mean) (mgh rstd^2)
+    const float mr = mg * rstd, mr2 = mgh * rstd * rstd;
     float t[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float h = (vs[j] - mean) * rstd;
-        t[j] = rstd * (vy[j] * gamma[j] - mg - h * mgh);
-    }
+    for (int j = 0; j < 8; ++j) t[j] = vy[j] * gamma[j] * rstd - mr - (vs[j] - mean) * mr2;
     if (ADD) {
         if (a.dsum.p)
 #pragma unroll
@@ -355,13 +354,14 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
                 r.fit(k, exact, vs[k]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float h = (vs[k][j] - mean) * rstd, y = vy[k][j], g = y * gamma[k][j];
+                    const float d = vs[k][j] - mean, y = vy[k][j], g = y * gamma[k][j];
                     sg += g;
-                    sgh += g * h;
-                    dg[k][j] += y * h;
+                    sgh += g * d;
+                    dg[k][j] += y * rstd * d;
                     db[k][j] += y;
                 }
             }
+            sgh *= rstd;
         }
         sg = sum_lanes<(G < 64 ? G : 64)>(sg);
         sgh = sum_lanes<(G < 64 ? G : 64)>(sgh);
@@ -385,8 +385,10 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (r.channel(k) >= a.c) continue;
-            vy[k].forget();
-            vs[k].forget();
+            if (ADD) {                                  // (where no registers are left for the values)
+                vy[k].forget();
+                vs[k].forget();
+            }
             if (ADD && a.dsum.p) r.fit(k, exact, vd[ADD ? k : 0]);
             put_gradients<ADD>(r, a, counter, row0, k, vy[k], vs[k], vd[ADD ? k : 0], gamma[k], mean, rstd, mg, mgh);
         }
