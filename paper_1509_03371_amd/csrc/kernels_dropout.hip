@@ -5,6 +5,10 @@ namespace sk {
 
 namespace {
 
+// One call of the generator, some sixty instructions of which twenty are products at a quarter of the rate, serves the eight channels of an octet: about half of the time
+// that 16-bit elements take to come and go.  HBM bounds it: 200 maps of 512^2 fp32 419 MB in 72 us = 5.8 TB/s, 64 x 388^2 bf16 of four images 154 MB in 30 us = 5.1.
+// (One call and one element a thread took 216 us for the first.)
+
 // A thread takes the eight channels of an octet that one call of the generator serves; 1 << shift octets of a row lie side by side in a workgroup.
 template <int DT> __global__ __launch_bounds__(256) void dropout_rows_kernel(DropoutArgs a, int shift, int parts)
 {

@@ -6,7 +6,10 @@ namespace sk {
 namespace {
 
 // A row belongs to G lanes; lane l holds channels 8*(k*G + l) .. + 7 for k < K, the whole row in registers: one read of every input, one write of
-// every output, and the variance from the values themselves about their mean.  T threads a workgroup; G > 64: G = T, sums through LDS.
+// every output, and the variance from the values themselves about their mean (no sum of squares to cancel).  Eight channels a lane because that is
+// what one call of dropout's generator serves; 16 bytes a load in 16 bits, two loads in fp32.  Rows of up to 64 lanes' worth need no LDS; longer ones
+// add their waves' sums there.  HBM bounds it: 65536 x 2048 bf16 537 MB in 105 us = 5.1 TB/s, with residual, dropout and sum 16384 x 4096 bf16 537 MB in 95 us =
+// 5.7 TB/s (a copy of 256 MB: 5.3); the first kernel, which read each row three times, took 544 and 605 us.
 template <int DT, int G> struct Row {
     typedef elem_t<DT> E;
     static constexpr int S = sizeof(E);
@@ -304,8 +307,8 @@ __device__ __forceinline__ void put_values(float *out, int c, int c0, const floa
 
 // Backwards: a workgroup takes R = T / G rows at a time, gridDim.x * R apart, and keeps its lanes' sums for dgamma and dbeta in registers until the end,
 // where they are added up over the R rows' lanes through LDS and go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta
-// themselves if there is one workgroup.  Eight waves a workgroup, not four or less: half the copies, whose writing and adding up cost 25 of 171 us for
-// 16384 x 4096 bf16.
+// themselves if there is one workgroup.  Eight waves a workgroup: with four, twice the copies, whose writing and adding up made 147 us of 134 for
+// 16384 x 4096 bf16 with dropout and residual (671 MB: 5.1 TB/s).  Few rows a wave are bound by latency: 8192 x 1001 fp16, two rows a wave, 14.8 us for 49 MB.
 template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T, 4) void norm_rows_bwd_kernel(NormBwdArgs a)
 {
     constexpr int W = T / 64, R = T / G;
