@@ -17,14 +17,10 @@ __device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, c
     const bool drops = ADD && a.drop.thresh && a.dx.p;
     uint32_t w[V][4];
     if (drops) t.draw(a.drop, counter, o0 + t.delta, w);
-    // rstd (gamma dy - mg - h mgh) with h = (s - mean) rstd, as dy (gamma rstd) - mg rstd - (s - mean) (mgh rstd^2)
-    float mr[V], mr2[V];
+    float mr[V];                                        // rstd (gamma dy - mg - h mgh) with h = (s - mean) rstd
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        mr[v] = mg[v] * rstd[v];
-        mr2[v] = mgh[v] * rstd[v] * rstd[v];
-    }
-    auto gradient = [&](int j, int v) { return vy.at(j, v) * (gamma[j] * rstd[v]) - mr[v] - (vs.at(j, v) - mean[v]) * mr2[v]; };
+    for (int v = 0; v < V; ++v) mr[v] = mgh[v] * rstd[v];
+    auto gradient = [&](int j, int v) { return rstd[v] * (product(vy.at(j, v), gamma[j]) - mg[v] - (vs.at(j, v) - mean[v]) * mr[v]); };
     auto to_x = [&](int j, int v, float f) {
         if (drops) f = dropped(f, w[v], j, a.drop);
         if (a.relu_x) f = vs.at(j, v) > 0.f ? f : 0.f;
@@ -55,6 +51,36 @@ __device__ __forceinline__ void put_gradients(const Tile<DT, LAYOUT, P, V> &t, c
     }
 }
 
+// dgamma and dbeta of octet o by a wave, over the tiles first, first + step, ... of its 64 * V pixels; the sums in every lane
+template <int DT, int LAYOUT, int V>
+__device__ __forceinline__ void norm_planes_sums(const NormBwdArgs &a, int o, long first, long step, long tiles, long row, float (&g)[8], float (&s)[8])
+{
+    Tile<DT, LAYOUT, 64, V> t(a.plane, row, tiles, a.c);
+    float dg[8] = {}, db[8] = {};
+    for (long tile = first; tile < tiles; tile += step) {
+        t.go(tile);
+        typename Tile<DT, LAYOUT, 64, V>::Octet vy, vs;
+        float mean[V], rstd[V];
+        t.load(a.dy, o, vy);
+        t.load(a.s, o, vs);
+        t.statistics(a.mean, mean);
+        t.statistics(a.rstd, rstd);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float mine = t.own(v) ? vy.at(j, v) : 0.f;
+                dg[j] += mine * ((vs.at(j, v) - mean[v]) * rstd[v]);
+                db[j] += mine;
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        g[j] = sum_lanes<64>(dg[j]);
+        s[j] = sum_lanes<64>(db[j]);
+    }
+}
+
 // pixels of a thread: four while it may have 256 registers, else two
 constexpr int bwd_pixels(int threads) { return threads == 1024 ? 2 : 4; }
 
@@ -63,8 +89,34 @@ constexpr int bwd_pixels(int threads) { return threads == 1024 ? 2 : 4; }
 // 4 x 64 x 388^2 bf16: 236 MB in 59 us, the sums of 512 copies (4.7 us) with it = 4.0 TB/s; planes of 128-byte multiples 43 us + 4.7, these begin at any
 // multiple of 32, and their segments touch a fifth line in four.  What did not help: the next tile's loads in flight (57.5 us for 57.1), 64-pixel
 // segments without a barrier (68), 512-byte segments (68: one workgroup a CU).
-template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(NormBwdArgs a, long tiles, long row)
+//
+// ROLES, for few pixels: the first `walkers` workgroups leave the sums alone, and each of the others takes them for an octet over all pixels, which are
+// read twice (from the L2): one launch and no workspace.
+
+template <int DT, int LAYOUT, int P, int T, bool ADD, bool ROLES>
+__global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(NormBwdArgs a, long tiles, long row, int walkers)
 {
+    if (ROLES && blockIdx.x >= (unsigned)walkers) {
+        __shared__ float sums[T / 64][16];
+        const long wide = (a.plane + 255) / 256;        // tiles of a wave's 64 * 4 pixels
+        const int o = blockIdx.x - walkers, wave = uniform(threadIdx.x >> 6), waves = blockDim.x >> 6;
+        float g[8], s[8];
+        norm_planes_sums<DT, LAYOUT, 4>(a, o, wave, waves, a.n * wide, wide, g, s);
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sums[wave][j] = g[j];
+                sums[wave][8 + j] = s[j];
+            }
+        __syncthreads();
+        const int c = 8 * o + (threadIdx.x & 7);
+        float *out = threadIdx.x < 8 ? a.dgamma : a.dbeta;
+        if (threadIdx.x >= 16 || c >= a.c || !out) return;
+        float v = 0.f;
+        for (int i = 0; i < waves; ++i) v += sums[i][threadIdx.x];
+        out[c] = v;
+        return;
+    }
     constexpr int V = bwd_pixels(T);
     extern __shared__ __align__(16) float part[];
     Tile<DT, LAYOUT, P, V> t(a.plane, row, tiles, a.c);
@@ -78,7 +130,7 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
         dg[j] = db[j] = 0.f;
     }
     int half = 0;
-    for (long tile = neighbour(); tile < tiles; tile += gridDim.x) {
+    for (long tile = ROLES ? blockIdx.x : neighbour(); tile < tiles; tile += walkers) {
         t.go(tile);
         typename Tile<DT, LAYOUT, P, V>::Octet vy, vs;
         t.load(a.dy, t.oct0, vy);
@@ -96,9 +148,10 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float d = vs.at(j, v) - mean[v], y = vy.at(j, v), g = y * gamma[j];
+                const float d = vs.at(j, v) - mean[v], y = vy.at(j, v), g = product(y, gamma[j]);
                 sums[0][v] += g;
                 sums[1][v] += g * d;
+                if (ROLES) continue;
                 dg[j] += y * r_once[v] * d;
                 db[j] += y * once[v];
             }
@@ -116,7 +169,7 @@ template <int DT, int LAYOUT, int P, int T, bool ADD> __global__ __launch_bounds
         }
         put_gradients<ADD>(t, a, counter, t.oct0, vy, vs, gamma, mean, rstd, mg, mgh);
     }
-    if (!a.dgamma && !a.dbeta) return;
+    if (ROLES || (!a.dgamma && !a.dbeta)) return;
     // an octet belongs to the P lanes that hold its pixels
     const bool alone = gridDim.x == 1;
     const long cp = norm_copy_floats(a.c) / 2;
@@ -166,7 +219,7 @@ template <int DT, int LAYOUT, int P, int V> __global__ __launch_bounds__(1024) v
                 float q = 0.f, r = 0.f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float g = vy.at(j, v) * gamma[j];
+                    const float g = product(vy.at(j, v), gamma[j]);
                     q += g;
                     r += g * ((vs.at(j, v) - mean[v]) * rstd[v]);
                 }
@@ -190,49 +243,41 @@ template <int DT, int LAYOUT, int P, int V> __global__ __launch_bounds__(1024) v
 // ... a wave an octet of channels, blockIdx.y a share of the tiles
 template <int DT, int LAYOUT, int V> __global__ __launch_bounds__(64) void norm_deep_planes_wgrad_kernel(NormBwdArgs a, long tiles, long row)
 {
-    Tile<DT, LAYOUT, 64, V> t(a.plane, row, tiles, a.c);
     const long cp = norm_copy_floats(a.c) / 2;
+    float *dgamma = gridDim.y == 1 ? a.dgamma : a.scratch + blockIdx.y * 2L * cp;
+    float *dbeta = gridDim.y == 1 ? a.dbeta : a.scratch + (blockIdx.y * 2L + 1) * cp;
     for (int o = blockIdx.x; 8 * o < a.c; o += gridDim.x) {
-        float dg[8] = {}, db[8] = {};
-        for (long tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
-            t.go(tile);
-            typename Tile<DT, LAYOUT, 64, V>::Octet vy, vs;
-            float mean[V], rstd[V];
-            t.load(a.dy, o, vy);
-            t.load(a.s, o, vs);
-            t.statistics(a.mean, mean);
-            t.statistics(a.rstd, rstd);
+        float g[8], s[8];
+        norm_planes_sums<DT, LAYOUT, V>(a, o, blockIdx.y, gridDim.y, tiles, row, g, s);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float mine = t.own(v) ? vy.at(j, v) : 0.f;
-                    dg[j] += mine * ((vs.at(j, v) - mean[v]) * rstd[v]);
-                    db[j] += mine;
-                }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float g = sum_lanes<64>(dg[j]), s = sum_lanes<64>(db[j]);
-            if (t.lane == 0 && 8 * o + j < a.c) {
-                float *dgamma = gridDim.y == 1 ? a.dgamma : a.scratch + blockIdx.y * 2L * cp;
-                float *dbeta = gridDim.y == 1 ? a.dbeta : a.scratch + (blockIdx.y * 2L + 1) * cp;
-                if (dgamma) dgamma[8 * o + j] = g;
-                if (dbeta) dbeta[8 * o + j] = s;
+        for (int j = 0; j < 8; ++j)
+            if (threadIdx.x == 0 && 8 * o + j < a.c) {
+                if (dgamma) dgamma[8 * o + j] = g[j];
+                if (dbeta) dbeta[8 * o + j] = s[j];
             }
-        }
     }
 }
 
 }  // namespace
 
+// Where ROLES take the work: up to sixteen tiles of 256 pixels and 2^21 elements.  With roles and with copies and a second launch, us, bf16: 64 x 128 4.1 and 4.9,
+// 1024 x 784 6.0 and 9.6, 64 x 4096 6.4 and 7.4, 256 x 4096 6.5 and 8.2, 1024 x 2000 9.6 and 10.5; 64 x 8192 10.2 and 7.5, 256 x 8192 11.1 and 9.1,
+// 1024 x 4096 20.5 and 13.3.
+static bool takes_roles(const NormSpan &s)
+{
+    return (s.layout == OCTETS || s.plane >= 4) && (s.c + 7) / 8 <= 256 && s.n * tiles_of_image(s, 256) <= 16 && s.n * s.plane * s.c <= 1L << 21;
+}
+// workgroups that the registers hold at once
+static int resident(int t, int threads) { return 256 * std::max(1, (t == 1024 ? 16 : 8) / (threads / 64)); }
+
 // (a call whose strides 32 bits do not span takes fewer: it walks octets, whose copies are at most 16)
 int norm_planes_bwd_copies(const NormSpan &s)
 {
     int copies = 16;
+    if (takes_roles(s)) return 1;
     if (s.layout == OCTETS || s.plane >= 4)
         pick_planes<true>(s.c, [&](auto p, auto t, int threads) {
-            copies = (int)std::min<long>(s.n * tiles_of_image(s, p() * bwd_pixels(t())), 256 * std::max(1, (t() == 1024 ? 16 : 8) / (threads / 64)));
+            copies = (int)std::min<long>(s.n * tiles_of_image(s, p() * bwd_pixels(t())), resident(t(), threads));
         });
     return copies;
 }
@@ -240,7 +285,7 @@ int norm_planes_bwd_copies(const NormSpan &s)
 hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t stream)
 {
     auto fits = [&](int p) { return spans(a, p, {&a.dy, &a.s, &a.dsum, &a.dx, &a.dresidual}); };
-    const bool sums = a.dgamma || a.dbeta, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
+    const bool sums = a.dgamma || a.dbeta, results = a.dx.p || a.dresidual.p, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
     pick_type(a, [&](auto dt, auto layout) {
         bool done = false;
         if (layout() == OCTETS || a.plane >= 4)
@@ -248,10 +293,21 @@ hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t 
                 if (!fits(p())) return;
                 const long row = tiles_of_image(a, p() * bwd_pixels(t())), tiles = a.n * row;
                 const size_t lds = part_bytes(2, p(), bwd_pixels(t()), threads);
-                if (adds) norm_planes_bwd_kernel<dt(), layout(), p(), t(), true><<<copies, threads, lds, stream>>>(a, tiles, row);
-                else norm_planes_bwd_kernel<dt(), layout(), p(), t(), false><<<copies, threads, lds, stream>>>(a, tiles, row);
-                if (sums && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
                 done = true;
+                const int all = (int)std::min<long>(tiles, resident(t(), threads));
+                const bool roles = sums && takes_roles(a);
+                if (roles) {
+                    const int walkers = results && !a.in_place() ? all : 0, blocks = walkers + (a.c + 7) / 8;
+                    if (adds) norm_planes_bwd_kernel<dt(), layout(), p(), t(), true, true><<<blocks, threads, lds, stream>>>(a, tiles, row, walkers);
+                    else norm_planes_bwd_kernel<dt(), layout(), p(), t(), false, true><<<blocks, threads, lds, stream>>>(a, tiles, row, walkers);
+                    if (walkers || !results) return;
+                }
+                NormBwdArgs b = a;
+                if (roles) b.dgamma = b.dbeta = nullptr;
+                if (roles || !sums) copies = all;
+                if (adds) norm_planes_bwd_kernel<dt(), layout(), p(), t(), true, false><<<copies, threads, lds, stream>>>(b, tiles, row, copies);
+                else norm_planes_bwd_kernel<dt(), layout(), p(), t(), false, false><<<copies, threads, lds, stream>>>(b, tiles, row, copies);
+                if (sums && !roles && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
             });
         if (done) return;
         pick_deep(a, !fits(4), [&](auto p, auto v) {
@@ -261,7 +317,7 @@ hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t 
                 norm_deep_planes_wgrad_kernel<dt(), layout(), v()><<<dim3(std::min((a.c + 7) / 8, 65536), shares), 64, 0, stream>>>(a, tiles, row);
                 if (shares > 1) (void)launch_norm_reduce(a.scratch, shares, a.dgamma, a.dbeta, a.c, stream);
             }
-            if (!a.dx.p && !a.dresidual.p) return;
+            if (!results) return;
             const long row = tiles_of_image(a, p() * v()), tiles = a.n * row;
             const int threads = deep_threads(a.c, p());
             norm_deep_planes_bwd_kernel<dt(), layout(), p(), v()><<<norm_blocks(tiles, 1), threads, part_bytes(2, p(), v(), threads), stream>>>(a, tiles, row);

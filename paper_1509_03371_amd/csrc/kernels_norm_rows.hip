@@ -272,11 +272,10 @@ __device__ __forceinline__ void put_gradients(const Row<DT, G> &r, const NormBwd
                                               const Words<DT, 8> &vs, const Words<DT, 8> &vd, const float (&gamma)[8], float mean, float rstd, float mg,
                                               float mgh)
 {
-    // rstd (gamma dy - mg - h mgh) with h = (s - mean) rstd, as (gamma dy) rstd - mg rstd - (s - mean) (mgh rstd^2)
-    const float mr = mg * rstd, mr2 = mgh * rstd * rstd;
+    const float mr = mgh * rstd;                        // rstd (gamma dy - mg - h mgh) with h = (s - mean) rstd
     float t[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = vy[j] * gamma[j] * rstd - mr - (vs[j] - mean) * mr2;
+    for (int j = 0; j < 8; ++j) t[j] = rstd * (product(vy[j], gamma[j]) - mg - (vs[j] - mean) * mr);
     if (ADD) {
         if (a.dsum.p)
 #pragma unroll
@@ -309,8 +308,54 @@ __device__ __forceinline__ void put_values(float *out, int c, int c0, const floa
 // where they are added up over the R rows' lanes through LDS and go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta
 // themselves if there is one workgroup.  Eight waves a workgroup: with four, twice the copies, whose writing and adding up made 147 us of 134 for
 // 16384 x 4096 bf16 with dropout and residual (671 MB: 5.1 TB/s).  Few rows a wave are bound by latency: 8192 x 1001 fp16, two rows a wave, 14.8 us for 49 MB.
-template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T, 4) void norm_rows_bwd_kernel(NormBwdArgs a)
+//
+// ROLES, for few rows: the first `walkers` workgroups leave the sums alone, and each of the others takes them for 64 channels over all rows, which are read twice
+// (from the L2): one launch and no workspace.
+template <int DT, int T> __device__ void norm_rows_sums(const NormBwdArgs &a, int block)
 {
+    constexpr int W = T / 64;
+    __shared__ float sums[W][2][64];
+    const Row<DT, 8> r(a.c);                            // eight lanes an octet each, eight rows a wave
+    const int wave = uniform(threadIdx.x >> 6);
+    float dg[8] = {}, db[8] = {};
+    for (long row0 = 8 * wave; row0 < a.n; row0 += 8 * W) {
+        if (row0 + r.sub >= a.n) break;
+        Words<DT, 8> vy, vs;
+        r.load(r.from(a.dy, row0), r.offset(a.dy), block, vy);
+        r.load(r.from(a.s, row0), r.offset(a.s), block, vs);
+        const float mean = a.mean[row0 + r.sub], rstd = a.rstd[row0 + r.sub];
+        r.fit(block, false, vy);
+        r.fit(block, false, vs);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            dg[j] += vy[j] * rstd * (vs[j] - mean);
+            db[j] += vy[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float g = sum_over_groups<8>(dg[j]), b = sum_over_groups<8>(db[j]);
+        if ((threadIdx.x & 63) < 8) {
+            sums[wave][0][8 * r.lane + j] = g;
+            sums[wave][1][8 * r.lane + j] = b;
+        }
+    }
+    __syncthreads();
+    const int which = threadIdx.x >> 6, c = block * 64 + (threadIdx.x & 63);
+    float *out = which ? a.dbeta : a.dgamma;
+    if (which > 1 || c >= a.c || !out) return;
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v += sums[i][which][threadIdx.x & 63];
+    out[c] = v;
+}
+
+template <int DT, int G, int K, int T, bool ADD, bool ROLES> __global__ __launch_bounds__(T, 4) void norm_rows_bwd_kernel(NormBwdArgs a, int walkers)
+{
+    if (ROLES && blockIdx.x >= (unsigned)walkers) {
+        norm_rows_sums<DT, T>(a, blockIdx.x - walkers);
+        return;
+    }
     constexpr int W = T / 64, R = T / G;
     constexpr int each = G < 64 ? 1 : G / 64;           // waves that hold one row's channels
     __shared__ float part[G > 64 ? 4 * W : 1];
@@ -334,7 +379,7 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
         }
     }
     int half = 0;
-    for (long first = blockIdx.x * (long)R; first < a.n; first += gridDim.x * (long)R) {     // (every thread alike)
+    for (long first = blockIdx.x * (long)R; first < a.n; first += walkers * (long)R) {     // (every thread alike)
         const long row0 = first + (G < 64 ? wave * (64 / G) : group);
         const bool mine = row0 + r.sub < a.n;
         if (G <= 64 && !mine) continue;                 // (G > 64: all come to the barrier)
@@ -357,9 +402,10 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
                 r.fit(k, exact, vs[k]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float d = vs[k][j] - mean, y = vy[k][j], g = y * gamma[k][j];
+                    const float d = vs[k][j] - mean, y = vy[k][j], g = product(y, gamma[k][j]);
                     sg += g;
                     sgh += g * d;
+                    if (ROLES) continue;
                     dg[k][j] += y * rstd * d;
                     db[k][j] += y;
                 }
@@ -396,7 +442,7 @@ template <int DT, int G, int K, int T, bool ADD> __global__ __launch_bounds__(T,
             put_gradients<ADD>(r, a, counter, row0, k, vy[k], vs[k], vd[ADD ? k : 0], gamma[k], mean, rstd, mg, mgh);
         }
     }
-    if (!a.dgamma && !a.dbeta) return;
+    if (ROLES || (!a.dgamma && !a.dbeta)) return;
     const bool alone = gridDim.x == 1;
     const long cp = norm_copy_floats(a.c) / 2;
     auto put = [&](const float (&acc)[K][8], float *own, int which) {
@@ -456,8 +502,9 @@ template <int DT> __global__ __launch_bounds__(1024) void norm_long_rows_bwd_ker
             float t0 = 0.f, t1 = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                t0 += vy[j] * gamma[j];
-                t1 += vy[j] * gamma[j] * ((vs[j] - mean) * rstd);
+                const float g = product(vy[j], gamma[j]);
+                t0 += g;
+                t1 += g * ((vs[j] - mean) * rstd);
             }
             sg += t0;
             sgh += t1;
@@ -608,18 +655,20 @@ hipError_t launch_norm_rows(const NormArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Rounds of rows that one workgroup takes alone, which then writes the sums themselves: no second launch, no workspace.  Alone and shared out, us: two rounds
-// (16 rows of 777 channels) 7.3 and 8.2, 4 x 4096 7.6 and 8.5; three (24 x 777) 8.5 and 8.2, five (37 x 777) 10.9 and 8.2.
-constexpr long kAloneRounds = 2;
+// Where ROLES take the work: up to 512 rows, 1024 of more than 2048 channels.  With roles and with copies and a second launch, us, bf16: 1 x 777 3.4 and 5.0, 37 x
+// 777 4.3 and 8.5, 512 x 777 7.2 and 9.0, 512 x 64 4.9 and 6.5, 1024 x 4096 11.2 and 21.3; 1024 x 777 10.9 and 9.6, 2048 x 64 11.3 and 6.7, 2048 x 4096 23.9
+// and 22.5.
+static bool takes_roles(const NormSpan &s) { return s.c > 8 && s.c <= kLongRowBwd && s.n <= (s.c > 2048 ? 1024 : 512); }
 
 // (rows far apart take as many: their workgroups hold no more of them)
 int norm_rows_bwd_copies(const NormSpan &s)
 {
     if (s.c > kLongRowBwd) return (int)std::min<long>(s.n, 16);
     int copies = 1;
+    if (takes_roles(s)) return copies;
     pick_rows_bwd(s.c, false, [&](auto g, auto, auto t) {
         const long rounds = (s.n + t() / g() - 1) / (t() / g());
-        copies = rounds <= kAloneRounds ? 1 : (int)std::min<long>(rounds, 256 * 1024 / t());
+        copies = (int)std::min<long>(rounds, 256 * 1024 / t());
     });
     return copies;
 }
@@ -627,7 +676,7 @@ int norm_rows_bwd_copies(const NormSpan &s)
 hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t stream)
 {
     if (a.relu_x) return hipErrorInvalidValue;
-    const bool sums = a.dgamma || a.dbeta, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
+    const bool sums = a.dgamma || a.dbeta, results = a.dx.p || a.dresidual.p, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
     const bool far = far_apart({&a.dy, &a.s, &a.dsum, &a.dx, &a.dresidual});
     pick_type(a.dtype, [&](auto dt) {
         if (a.c > kLongRowBwd) {
@@ -635,13 +684,25 @@ hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t st
                 norm_long_rows_wgrad_kernel<dt()><<<dim3((unsigned)std::min((a.c + 8191) / 8192, 65536), copies), 1024, 0, stream>>>(a);
                 if (copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
             }
-            if (a.dx.p || a.dresidual.p) norm_long_rows_bwd_kernel<dt()><<<norm_blocks(a.n, 1), 1024, 0, stream>>>(a);
+            if (results) norm_long_rows_bwd_kernel<dt()><<<norm_blocks(a.n, 1), 1024, 0, stream>>>(a);
             return;
         }
         pick_rows_bwd(a.c, far, [&](auto g, auto k, auto t) {
-            if (adds) norm_rows_bwd_kernel<dt(), g(), k(), t(), true><<<copies, t(), 0, stream>>>(a);
-            else norm_rows_bwd_kernel<dt(), g(), k(), t(), false><<<copies, t(), 0, stream>>>(a);
-            if (sums && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
+            const long rounds = (a.n + t() / g() - 1) / (t() / g());
+            const int all = (int)std::min<long>(rounds, 256 * 1024 / t());
+            const bool roles = sums && !far && takes_roles(a);
+            if (roles) {
+                const int walkers = results && !a.in_place() ? all : 0, blocks = walkers + (a.c + 63) / 64;
+                if (adds) norm_rows_bwd_kernel<dt(), g(), k(), t(), true, true><<<blocks, t(), 0, stream>>>(a, walkers);
+                else norm_rows_bwd_kernel<dt(), g(), k(), t(), false, true><<<blocks, t(), 0, stream>>>(a, walkers);
+                if (walkers || !results) return;
+            }
+            NormBwdArgs b = a;
+            if (roles) b.dgamma = b.dbeta = nullptr;
+            if (roles || !sums) copies = all;
+            if (adds) norm_rows_bwd_kernel<dt(), g(), k(), t(), true, false><<<copies, t(), 0, stream>>>(b, copies);
+            else norm_rows_bwd_kernel<dt(), g(), k(), t(), false, false><<<copies, t(), 0, stream>>>(b, copies);
+            if (sums && !roles && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
         });
     });
     return hipGetLastError();

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "philox.h"
 
 namespace sk {
@@ -50,6 +52,13 @@ struct NormBwdArgs : NormSpan {
     size_t scratch_floats;
     int relu_x;
     DropMask drop;
+    // does a result go to the place of what the parameters' sums are made from?
+    bool in_place() const
+    {
+        for (const void *out : {dx.p, dresidual.p})
+            if (out && (out == dy.p || out == s.p)) return true;
+        return false;
+    }
 };
 size_t norm_bwd_scratch_floats(const NormSpan &s);        // of the fastest launch; with less, fewer workgroups share the sums out
 hipError_t launch_layer_norm_bwd(const NormBwdArgs &a, hipStream_t stream);

@@ -44,6 +44,14 @@ template <int DT, int N> __device__ __forceinline__ void store_at(dst_t base, ui
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// a * b, rounded: never part of a fused operation.  gamma * dy minus its mean has to vanish where they are equal (one channel), as it does not if one of
+// the two is the unrounded product.
+__device__ __forceinline__ float product(float a, float b)
+{
+#pragma clang fp contract(off)
+    return a * b;
+}
+
 // N elements as the words that hold them, which is how they stay in registers: 16-bit ones are widened at each use
 template <int DT, int N> struct Words {
     static constexpr int count = (N * (DT == 0 ? 4 : 2) + 3) / 4;

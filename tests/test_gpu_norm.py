@@ -382,3 +382,19 @@ def test_small_planes_and_many_channels(shape):
     close(dres, t, rounded(t, "f32", et), "dresidual")
     close(dg, rg, eg, "dgamma")
     close(db, rb, eb, "dbeta")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("shape", [(3000, 1), (40, 1), (1, 1, 900), (3, 1, 5), (2, 1, 70000)], ids=str)
+def test_one_channel_has_no_gradient(shape, kind):
+    # (s - mean) and (gamma dy - its mean) are zero, not nearly
+    from paper_1509_03371_amd import binding as B
+    x, _, _, beta, dy, dsum = inputs(shape, kind, 3)
+    x, dy, dsum = (place(a, kind) for a in (x, dy, dsum))
+    gamma = torch.full((1,), 1.2345678, device="cuda")
+    y, s, mean, rstd = B.layer_norm(x, gamma, torch.from_numpy(beta).cuda(), axis=1)
+    assert torch.equal(y, torch.from_numpy(beta).cuda().to(y.dtype).expand(y.numel()).reshape(shape))
+    dx, _, dg, db = B.layer_norm_backward(dy, x, mean, rstd, gamma, axis=1)
+    assert (dx == 0).all() and (dg == 0).all() and (db != 0).all()
+    dx, dr, _, _ = B.layer_norm_backward(dy, x, mean, rstd, gamma, axis=1, dsum=dsum, p=0.5, seed=1)
+    assert torch.equal(dr, dsum) and torch.equal(dx, B.dropout(dsum, 0.5, 1, axis=1))

@@ -45,7 +45,12 @@ def data(n, c, h, w, classes, seed):
     return np.float32(rng.random((n, c, h, w))), lab
 
 
+WIDE = [S.conv(2056, 1, relu=False), S.norm(relu=True), S.dropout(0.1), S.conv(1100, 1), S.norm(), S.conv(520, 1, relu=False), S.dropout(0.2), S.norm(relu=True),
+        S.conv(260, 1), S.norm(), S.conv(2, 1, relu=False)]
+
 NETS_ = [(MIXED, 1, 2, 2, 31, 45), (ENDS, 3, 3, 1, 20, 33), (SINGLE, 2, 4, 2, 9, 30)]
+# layer by layer only: among 2056 x 117 samples in front of a ReLU some lie within fp32 rounding of zero, and a whole net's gradients then differ by those
+WIDE_ = (WIDE, 3, 2, 1, 9, 13)
 
 
 @pytest.mark.parametrize("layers,c_in,classes,n,h,w", NETS_, ids=["mixed", "ends", "single"])
@@ -96,7 +101,7 @@ def test_fp32_net_against_the_oracle(layers, c_in, classes, n, h, w):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("layers,c_in,classes,n,h,w", NETS_, ids=["mixed", "ends", "single"])
+@pytest.mark.parametrize("layers,c_in,classes,n,h,w", NETS_ + [WIDE_], ids=["mixed", "ends", "single", "wide"])
 def test_layers_on_the_maps_the_pass_stored(layers, c_in, classes, n, h, w, kind):
     net, _, _, norms = make(layers, c_in, kind, 51)
     img, lab = data(n, c_in, h, w, classes, 52)
@@ -273,5 +278,11 @@ def test_step_names_and_times(kind):
     names = [net.step_name(i) for i in range(net.num_steps())]
     assert "norm1" in names and "dropout3" in names and "conv10_k1_d1_o2" in names
     assert all(net.time_step(i, 2) >= 0 for i in range(len(names)))
+    y = torch.from_numpy(lab).cuda()
+    assert all(net.time_backward_step(y, i, 1, 2) >= 0 for i in (1, 3, 5, 8, 9))
+    from paper_1509_03371_amd import binding as B
+    for i in (1, 3):
+        with pytest.raises(B.SknetError):                   # part 0 is a convolution's
+            net.time_backward_step(y, i, 0, 2)
     assert net.get_dropout()[1] == 1                        # timing a step is no pass
     net.close()
