@@ -407,7 +407,8 @@ sk_status sknet3d_get_pool_argmax(sknet3d_t *net, int32_t pool_idx, int32_t *idx
  * parameter gradients.  Limits (SK_EUNSUPPORTED): 2^27 channels, 2^40 positions, 2^46 elements reached.
  *
  * In place: an output may be the tensor of an input, with the same strides.  SK_EINVAL for any other overlap of an output
- * with an input or another output, as far as views of one call go.
+ * with an input or another output, as far as views of one call go; the fp32 values that a call writes, and its workspace, must
+ * not overlap other fp32 values of the call (SK_EINVAL), nor its views.
  *
  * Everything is enqueued on hip_stream; the current HIP device must be that of the stream and the buffers.  Nothing is
  * allocated, kept or synchronised: calls can be recorded into a graph, and may overlap as long as their buffers do not. */
@@ -452,7 +453,8 @@ sk_status sknet_layer_norm(const sk_extent *extent, const sk_view *x, const sk_v
  *   dgamma = sum over positions of dy h;  dbeta = sum over positions of dy.
  * dsum: the gradient that reaches s from elsewhere, or NULL.  drop: the forward call's, or NULL.  dx, dresidual, dgamma_dev, dbeta_dev: each may
  * be NULL.  Sums are taken in a fixed order: equal calls give equal bits.  workspace_dev: DEVICE, 16-byte aligned, of at least
- * the bytes that sknet_layer_norm_workspace reports for the extent (NULL if neither dgamma nor dbeta is asked for), used until the call's work has run. */
+ * the bytes that sknet_layer_norm_workspace reports for the extent, used until the call's work has run (NULL where that is 0, as for small extents, or if
+ * neither dgamma nor dbeta is asked for). */
 sk_status sknet_layer_norm_workspace(const sk_extent *extent, uint64_t *bytes);
 sk_status sknet_layer_norm_backward(const sk_extent *extent, const sk_view *dy, const sk_view *s, const float *mean_dev, const float *rstd_dev,
                                     const float *gamma_dev, const sk_view *dsum, const sk_drop *drop, const sk_view *dx, const sk_view *dresidual,

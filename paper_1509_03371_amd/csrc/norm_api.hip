@@ -98,6 +98,30 @@ sk_status check_apart(const char *who, const sk_extent &e, const char *a_name, c
     return fail(SK_EINVAL, "%s: %s and %s overlap", who, a_name, b_name);
 }
 
+// fp32 values beside the views: parameters, statistics, their gradients
+struct Values {
+    const char *name;
+    const void *p;
+    int64_t bytes;
+    bool output;
+};
+
+// aligned to their elements, and what is written shares no place with the others
+template <int N>
+sk_status check_values(const char *who, const Values (&v)[N])
+{
+    for (const Values &a : v) {
+        if (reinterpret_cast<uintptr_t>(a.p) % 4) return fail(SK_EINVAL, "%s: %s is not aligned to its elements", who, a.name);
+        if (!a.p || !a.output) continue;
+        const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p);
+        for (const Values &b : v) {
+            const uintptr_t b0 = reinterpret_cast<uintptr_t>(b.p);
+            if (&a != &b && b.p && a0 < b0 + b.bytes && b0 < a0 + a.bytes) return fail(SK_EINVAL, "%s: %s and %s overlap", who, a.name, b.name);
+        }
+    }
+    return SK_OK;
+}
+
 sk_status take_mask(const char *who, const sk_drop *d, sk::DropMask *m)
 {
     if (!d) return SK_OK;
@@ -168,6 +192,9 @@ sk_status sknet_layer_norm(const sk_extent *extent, const sk_view *x, const sk_v
     SK_TRY(check_in_place(who, e, "y", y, "residual", residual));
     SK_TRY(check_in_place(who, e, "sum", sum, "x", x));
     SK_TRY(check_in_place(who, e, "sum", sum, "residual", residual));
+    const int64_t line = 4 * e.c, positions = 4 * e.n * e.plane;
+    const Values values[] = {{"gamma", gamma_dev, line, false}, {"beta", beta_dev, line, false}, {"mean", mean_dev, positions, true}, {"rstd", rstd_dev, positions, true}};
+    SK_TRY(check_values(who, values));
     take_span(e, &a);
     a.x = take_view(x);
     a.residual = take_view(residual);
@@ -219,6 +246,10 @@ sk_status sknet_layer_norm_backward(const sk_extent *extent, const sk_view *dy, 
         if (need && (!workspace_dev || workspace_bytes < need))
             return fail(SK_EINVAL, "%s: needs a workspace of %llu bytes", who, (unsigned long long)need);
         if (reinterpret_cast<uintptr_t>(workspace_dev) % 16) return fail(SK_EINVAL, "%s: the workspace is not aligned to 16 bytes", who);
+        const int64_t line = 4 * e.c, positions = 4 * e.n * e.plane;
+        const Values values[] = {{"mean", mean_dev, positions, false}, {"rstd", rstd_dev, positions, false}, {"gamma", gamma_dev, line, false},
+                                 {"dgamma", dgamma_dev, line, true}, {"dbeta", dbeta_dev, line, true}, {"the workspace", workspace_dev, (int64_t)need, true}};
+        SK_TRY(check_values(who, values));
         a.dy = take_view(dy);
         a.s = take_view(s);
         a.dsum = take_view(dsum);

@@ -123,10 +123,29 @@ def test_layer_norm_backward_refusals():
     need = C.c_uint64()
     big = extent(n=100000, c=64)
     assert B.lib.sknet_layer_norm_workspace(C.byref(big), C.byref(need)) == 0
+    assert need.value
     if need.value:
         assert go(e=big, dy=view(0x10000000, 64), s=view(0x20000000, 64), dx=view(0x30000000, 64), ws=0x40000000, n=need.value - 1) == "SK_EINVAL"
     assert status(B.lib.sknet_layer_norm_workspace, extent(c=0), C.byref(need)) == "SK_ESHAPE"
     assert status(B.lib.sknet_layer_norm_workspace, extent(), None) == "SK_EINVAL"
+
+
+def test_values_that_are_written_lie_apart():
+    def forward(gamma=0x50000, beta=0x60000, mean=0x70000, rstd=0x80000):
+        return status(B.lib.sknet_layer_norm, extent(), X, None, None, gamma, beta, 1e-5, None, Y, mean, rstd, None)
+
+    def backward(e=extent(), far=1, mean=0x50000, rstd=0x60000, gamma=0x70000, dgamma=0x80000, dbeta=0x90000, ws=None, n=0):
+        dy, s, dx = (view(a * far, e.c) for a in (0x10000, 0x20000, 0x30000))
+        return status(B.lib.sknet_layer_norm_backward, e, dy, s, mean, rstd, gamma, None, None, dx, None, dgamma, dbeta, ws, n, None)
+    # 4 means and 8 gammas: 16 and 32 bytes
+    assert forward(mean=0x80000) == forward(rstd=0x70000 + 12) == forward(mean=0x50000 + 28) == forward(rstd=0x60000 - 12) == "SK_EINVAL"
+    assert forward(gamma=0x50002) == forward(rstd=0x80001) == "SK_EINVAL"
+    assert backward(dgamma=0x90000) == backward(dbeta=0x80000 + 28) == backward(dgamma=0x70000) == backward(dbeta=0x50000 - 28) == "SK_EINVAL"
+    assert backward(dgamma=0x60000 + 12) == backward(gamma=0x70002) == backward(dbeta=0x90002) == "SK_EINVAL"
+    big, need = extent(n=100000, c=64), C.c_uint64()
+    assert B.lib.sknet_layer_norm_workspace(C.byref(big), C.byref(need)) == 0 and need.value > 256
+    spread = dict(e=big, far=0x1000, mean=0x60000000, rstd=0x70000000, gamma=0x80000000, dgamma=0x90000000, dbeta=0xa0000000, n=need.value)
+    assert backward(ws=0x90000000, **spread) == backward(ws=0x80000000, **spread) == backward(ws=0x60000000, **spread) == "SK_EINVAL"
 
 
 def test_calls_without_positions_do_nothing():
