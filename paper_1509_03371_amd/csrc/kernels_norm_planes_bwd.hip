@@ -86,7 +86,7 @@ constexpr int bwd_pixels(int threads) { return threads == 1024 ? 2 : 4; }
 
 // Backwards: a workgroup walks the tiles gridDim.x apart and keeps its threads' sums for dgamma and dbeta in registers until the end, where they go to the
 // workgroup's copy of the scratch, or to dgamma and dbeta themselves if there is one workgroup.  The grid is what fits the registers at once.
-// 4 x 64 x 388^2 bf16: 236 MB in 59 us, the sums of 512 copies (4.7 us) with it = 4.0 TB/s; planes of 128-byte multiples 43 us + 4.7, these begin at any
+// 4 x 64 x 388^2 bf16: 236 MB in 60 us, the sums of 512 copies (4.7 us) with it = 3.9 TB/s; planes of 128-byte multiples 43 us + 4.7, these begin at any
 // multiple of 32, and their segments touch a fifth line in four.  What did not help: the next tile's loads in flight (57.5 us for 57.1), 64-pixel
 // segments without a barrier (68), 512-byte segments (68: one workgroup a CU).
 //

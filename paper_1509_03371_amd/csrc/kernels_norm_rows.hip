@@ -307,7 +307,7 @@ __device__ __forceinline__ void put_values(float *out, int c, int c0, const floa
 // Backwards: a workgroup takes R = T / G rows at a time, gridDim.x * R apart, and keeps its lanes' sums for dgamma and dbeta in registers until the end,
 // where they are added up over the R rows' lanes through LDS and go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta
 // themselves if there is one workgroup.  Eight waves a workgroup: with four, twice the copies, whose writing and adding up made 147 us of 134 for
-// 16384 x 4096 bf16 with dropout and residual (671 MB: 5.1 TB/s).  Few rows a wave are bound by latency: 8192 x 1001 fp16, two rows a wave, 14.8 us for 49 MB.
+// 16384 x 4096 bf16 with dropout and residual (671 MB: 5.1 TB/s).  Few rows a wave are bound by latency: 8192 x 1001 fp16, two rows a wave, 15.3 us for 49 MB.
 //
 // ROLES, for few rows: the first `walkers` workgroups leave the sums alone, and each of the others takes them for 64 channels over all rows, which are read twice
 // (from the L2): one launch and no workspace.
