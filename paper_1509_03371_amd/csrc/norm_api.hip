@@ -1,5 +1,6 @@
 // Host side of the operators on a caller's tensors: dropout and layer norm.  See include/sknet.h for the contract.
 #include <cmath>
+#include <utility>
 
 #include "norm.h"
 #include "sk_host.h"
@@ -62,8 +63,24 @@ bool same_strides(const sk_extent &e, const sk_view &a, const sk_view &b)
     return (e.n == 1 || a.stride_n == b.stride_n) && (e.layout == SK_ROWS || e.c == 1 || a.stride_c == b.stride_c);
 }
 
-// Do two views share no element?  True where their ranges of memory are apart, or where they are windows of one buffer: equal strides, and the
-// distance between them, modulo a stride, leaves each window's extent below that stride outside the other's.
+// `len` places, `stride` bytes apart
+struct Steps {
+    __int128 len, stride;
+};
+
+// Is there an i of -(len - 1) .. len - 1 with f(far - i stride), which can hold only where its argument lies within (-reach, reach)?  Two at
+// most come into question: the places of a step lie at least `reach` apart.
+template <class F> bool some_step(__int128 far, const Steps &s, F f)
+{
+    if (s.len == 1) return f(far);
+    const __int128 down = far >= 0 ? far / s.stride : -((-far + s.stride - 1) / s.stride);
+    for (__int128 i = down; i <= down + 1; ++i)
+        if (i > -s.len && i < s.len && f(far - i * s.stride)) return true;
+    return false;
+}
+
+// Do two views share no element?  True where their ranges of memory are apart, and with equal strides where no difference i stride_n + j stride_c of two
+// places brings their lines together.  With equal strides one of the two must have elements apart (an output).
 bool disjoint(const sk_extent &e, const sk_view &a, const sk_view &b)
 {
     const int64_t size = element_bytes(e);
@@ -71,16 +88,11 @@ bool disjoint(const sk_extent &e, const sk_view &a, const sk_view &b)
     const __int128 a1 = a0 + (last_element(e, a) + 1) * size, b1 = b0 + (last_element(e, b) + 1) * size;
     if (a1 <= b0 || b1 <= a0) return true;
     if (!same_strides(e, a, b)) return false;
-    auto windows = [&](__int128 stride, __int128 extent) {
-        if (stride <= 0) return false;
-        const __int128 far = (b0 > a0 ? b0 - a0 : a0 - b0) % (stride * size);
-        return far >= extent * size && stride * size - far >= extent * size;
-    };
-    if (e.layout == SK_ROWS) return e.n > 1 && windows(a.stride_n, e.c);
-    const bool images_outside = a.stride_n >= a.stride_c;
-    const __int128 per_map = images_outside ? e.plane : (__int128)(e.n - 1) * a.stride_n + e.plane;
-    const __int128 per_image = images_outside ? (__int128)(e.c - 1) * a.stride_c + e.plane : e.plane;
-    return (e.c > 1 && windows(a.stride_c, per_map)) || (e.n > 1 && windows(a.stride_n, per_image));
+    const bool rows = e.layout == SK_ROWS;
+    const __int128 line = (rows ? e.c : e.plane) * (__int128)size;
+    Steps images = {e.n, e.n == 1 ? 0 : (__int128)a.stride_n * size}, maps = {rows || e.c == 1 ? 1 : e.c, rows || e.c == 1 ? 0 : (__int128)a.stride_c * size};
+    if (images.stride < maps.stride) std::swap(images, maps);       // the wider step first: it spans all of the other's
+    return !some_step(b0 - a0, images, [&](__int128 r) { return some_step(r, maps, [&](__int128 d) { return d > -line && d < line; }); });
 }
 
 // an output may be an input's buffer, element for element; any other overlap is refused
