@@ -286,36 +286,37 @@ hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t 
 {
     auto fits = [&](int p) { return spans(a, p, {&a.dy, &a.s, &a.dsum, &a.dx, &a.dresidual}); };
     const bool sums = a.dgamma || a.dbeta, results = a.dx.p || a.dresidual.p, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
+    Launches done;
     pick_type(a, [&](auto dt, auto layout) {
-        bool done = false;
+        bool taken = false;
         if (layout() == OCTETS || a.plane >= 4)
             pick_planes<true>(a.c, [&](auto p, auto t, int threads) {
                 if (!fits(p())) return;
                 const long row = tiles_of_image(a, p() * bwd_pixels(t())), tiles = a.n * row;
                 const size_t lds = part_bytes(2, p(), bwd_pixels(t()), threads);
-                done = true;
+                taken = true;
                 const int all = (int)std::min<long>(tiles, resident(t(), threads));
                 const bool roles = sums && takes_roles(a);
                 if (roles) {
                     const int walkers = results && !a.in_place() ? all : 0, blocks = walkers + (a.c + 7) / 8;
                     if (adds) norm_planes_bwd_kernel<dt(), layout(), p(), t(), true, true><<<blocks, threads, lds, stream>>>(a, tiles, row, walkers);
                     else norm_planes_bwd_kernel<dt(), layout(), p(), t(), false, true><<<blocks, threads, lds, stream>>>(a, tiles, row, walkers);
-                    if (walkers || !results) return;
+                    if (done.failed() || walkers || !results) return;
                 }
                 NormBwdArgs b = a;
                 if (roles) b.dgamma = b.dbeta = nullptr;
                 if (roles || !sums) copies = all;
                 if (adds) norm_planes_bwd_kernel<dt(), layout(), p(), t(), true, false><<<copies, threads, lds, stream>>>(b, tiles, row, copies);
                 else norm_planes_bwd_kernel<dt(), layout(), p(), t(), false, false><<<copies, threads, lds, stream>>>(b, tiles, row, copies);
-                if (sums && !roles && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
+                if (!done.failed() && sums && !roles && copies > 1) done.failed(launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream));
             });
-        if (done) return;
+        if (taken) return;
         pick_deep(a, !fits(4), [&](auto p, auto v) {
             if (sums) {
                 const long row = tiles_of_image(a, 64 * v()), tiles = a.n * row;
                 const int shares = (int)std::min<long>(std::min(copies, 16), tiles);
                 norm_deep_planes_wgrad_kernel<dt(), layout(), v()><<<dim3(std::min((a.c + 7) / 8, 65536), shares), 64, 0, stream>>>(a, tiles, row);
-                if (shares > 1) (void)launch_norm_reduce(a.scratch, shares, a.dgamma, a.dbeta, a.c, stream);
+                if (done.failed() || (shares > 1 && done.failed(launch_norm_reduce(a.scratch, shares, a.dgamma, a.dbeta, a.c, stream)))) return;
             }
             if (!results) return;
             const long row = tiles_of_image(a, p() * v()), tiles = a.n * row;
@@ -323,7 +324,7 @@ hipError_t launch_norm_planes_bwd(const NormBwdArgs &a, int copies, hipStream_t 
             norm_deep_planes_bwd_kernel<dt(), layout(), p(), v()><<<norm_blocks(tiles, 1), threads, part_bytes(2, p(), v(), threads), stream>>>(a, tiles, row);
         });
     });
-    return hipGetLastError();
+    return done.status();
 }
 
 }  // namespace sk

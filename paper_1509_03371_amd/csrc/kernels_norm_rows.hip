@@ -678,11 +678,12 @@ hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t st
     if (a.relu_x) return hipErrorInvalidValue;
     const bool sums = a.dgamma || a.dbeta, results = a.dx.p || a.dresidual.p, adds = a.dsum.p || a.dresidual.p || a.drop.thresh;
     const bool far = far_apart({&a.dy, &a.s, &a.dsum, &a.dx, &a.dresidual});
+    Launches done;
     pick_type(a.dtype, [&](auto dt) {
         if (a.c > kLongRowBwd) {
             if (sums) {
                 norm_long_rows_wgrad_kernel<dt()><<<dim3((unsigned)std::min((a.c + 8191) / 8192, 65536), copies), 1024, 0, stream>>>(a);
-                if (copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
+                if (done.failed() || (copies > 1 && done.failed(launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream)))) return;
             }
             if (results) norm_long_rows_bwd_kernel<dt()><<<norm_blocks(a.n, 1), 1024, 0, stream>>>(a);
             return;
@@ -695,17 +696,17 @@ hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t st
                 const int walkers = results && !a.in_place() ? all : 0, blocks = walkers + (a.c + 63) / 64;
                 if (adds) norm_rows_bwd_kernel<dt(), g(), k(), t(), true, true><<<blocks, t(), 0, stream>>>(a, walkers);
                 else norm_rows_bwd_kernel<dt(), g(), k(), t(), false, true><<<blocks, t(), 0, stream>>>(a, walkers);
-                if (walkers || !results) return;
+                if (done.failed() || walkers || !results) return;
             }
             NormBwdArgs b = a;
             if (roles) b.dgamma = b.dbeta = nullptr;
             if (roles || !sums) copies = all;
             if (adds) norm_rows_bwd_kernel<dt(), g(), k(), t(), true, false><<<copies, t(), 0, stream>>>(b, copies);
             else norm_rows_bwd_kernel<dt(), g(), k(), t(), false, false><<<copies, t(), 0, stream>>>(b, copies);
-            if (sums && !roles && copies > 1) (void)launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream);
+            if (!done.failed() && sums && !roles && copies > 1) done.failed(launch_norm_reduce(a.scratch, copies, a.dgamma, a.dbeta, a.c, stream));
         });
     });
-    return hipGetLastError();
+    return done.status();
 }
 
 }  // namespace sk

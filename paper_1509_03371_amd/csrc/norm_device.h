@@ -154,6 +154,18 @@ inline unsigned norm_blocks(long work, long each)
     return (unsigned)(b < (1L << 21) ? b : 1L << 21);
 }
 
+// The first error of a call's launches: reading it clears it, so what a later launch reads says nothing of those before.
+struct Launches {
+    hipError_t first = hipSuccess;
+    bool failed(hipError_t e)
+    {
+        if (first == hipSuccess) first = e;
+        return first != hipSuccess;
+    }
+    bool failed() { return failed(hipGetLastError()); }         // with the launch just made
+    hipError_t status() { return failed() ? first : hipSuccess; }
+};
+
 // dgamma and dbeta from the `copies` copies of their sums, each [2][c rounded up to 4]
 hipError_t launch_norm_reduce(const float *scratch, int copies, float *dgamma, float *dbeta, int c, hipStream_t stream);
 __host__ __device__ inline long norm_copy_floats(long c) { return 2 * ((c + 3) / 4 * 4); }
