@@ -603,38 +603,43 @@ __global__ __launch_bounds__(256) void norm_reduce_kernel(const float *scratch, 
 {
     typedef float floatx4 __attribute__((ext_vector_type(4)));
     __shared__ floatx4 sh[4][4];
-    const int cp = (c + 3) / 4 * 4, e = blockIdx.x * 16 + 4 * (threadIdx.x & 3), group = threadIdx.x >> 2;
-    floatx4 s{};
-    if (e < 2 * cp) {
-        const float *p = scratch + e;
-        int i = group;
-        for (; i + 7 * 64 < copies; i += 8 * 64) {
-            floatx4 v[8];
+    const int cp = (c + 3) / 4 * 4, group = threadIdx.x >> 2;
+    for (int first = blockIdx.x * 16; first < 2 * cp; first += gridDim.x * 16) {        // (every thread alike)
+        const int e = first + 4 * (threadIdx.x & 3);
+        floatx4 s{};
+        if (e < 2 * cp) {
+            const float *p = scratch + e;
+            int i = group;
+            for (; i + 7 * 64 < copies; i += 8 * 64) {
+                floatx4 v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const floatx4 *>(p + (long)(i + 64 * u) * 2 * cp);
-            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+                for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const floatx4 *>(p + (long)(i + 64 * u) * 2 * cp);
+                s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            }
+            for (; i < copies; i += 64) s += *reinterpret_cast<const floatx4 *>(p + (long)i * 2 * cp);
         }
-        for (; i < copies; i += 64) s += *reinterpret_cast<const floatx4 *>(p + (long)i * 2 * cp);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = sum_over_groups<4>(s[j]);
+        if ((threadIdx.x & 63) < 4) sh[threadIdx.x >> 6][threadIdx.x & 3] = s;
+        __syncthreads();
+        if (threadIdx.x < 4 && e < 2 * cp) {
+            s = (sh[0][threadIdx.x] + sh[1][threadIdx.x]) + (sh[2][threadIdx.x] + sh[3][threadIdx.x]);
+            float *out = e < cp ? dgamma : dbeta;
+            const int k = e < cp ? e : e - cp;
+            if (out)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (k + j < c) out[k + j] = s[j];
+        }
+        __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s[j] = sum_over_groups<4>(s[j]);
-    if ((threadIdx.x & 63) < 4) sh[threadIdx.x >> 6][threadIdx.x & 3] = s;
-    __syncthreads();
-    if (threadIdx.x >= 4 || e >= 2 * cp) return;
-    s = (sh[0][threadIdx.x] + sh[1][threadIdx.x]) + (sh[2][threadIdx.x] + sh[3][threadIdx.x]);
-    float *out = e < cp ? dgamma : dbeta;
-    const int k = e < cp ? e : e - cp;
-    if (out)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (k + j < c) out[k + j] = s[j];
 }
 
 }  // namespace
 
 hipError_t launch_norm_reduce(const float *scratch, int copies, float *dgamma, float *dbeta, int c, hipStream_t stream)
 {
-    norm_reduce_kernel<<<(unsigned)((norm_copy_floats(c) + 15) / 16), 256, 0, stream>>>(scratch, copies, dgamma, dbeta, c);
+    norm_reduce_kernel<<<norm_blocks(norm_copy_floats(c), 16), 256, 0, stream>>>(scratch, copies, dgamma, dbeta, c);
     return hipGetLastError();
 }
 

@@ -99,3 +99,17 @@ def test_a_failed_launch_is_reported(program, name, dtype, adds, in_place):
     words = r.stdout.split()
     assert words[0] == "0:0" and "launches %d " % launches in r.stdout, r.stdout
     assert words[1:1 + launches] == ["%d:5" % (i + 1) for i in range(launches)], r.stdout       # SK_EDEVICE whichever it was
+
+
+EMPTY = {"no rows, the most channels": (ROWS, 0, 1 << 27, 1, 0, 1), "no pixels": (MAPS, 3, 1 << 27, 0, 0, 1), "many rows": (ROWS, 1 << 36, 8, 1, 0, 2),
+         "many rows of wide gaps": (ROWS, 1 << 26, 64, 1, 1 << 20, 2), "many images": (MAPS, 1 << 36, 9, 3, 0, 3), "one long plane": (MAPS, 1, 24, 1 << 36, 0, 2),
+         "the most channels of maps": (MAPS, 2, 1 << 27, 3, 0, 3)}
+
+
+@pytest.mark.parametrize("name", list(CALLS) + list(EMPTY))
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_grids_fit_a_launch(program, name, dtype):
+    # 2^32 - 1 threads along an axis: a workgroup of 256 for each sixteen of 2^28 sums would be one more
+    layout, n, c, plane, stride, launches = {**CALLS, **EMPTY}[name]
+    r = program(dtype, layout, n, c, plane, 0, 0, stride)
+    assert r.returncode == 0 and "launches %d too large 0" % launches in r.stdout, r.stdout
