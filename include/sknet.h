@@ -148,8 +148,10 @@ sk_status sknet_get_norm_grad(sknet_t *net, int32_t norm_idx, float *dgamma_host
 /* The masks of SK_DROPOUT layers: that of layer number l (0-based, of all layers) in the step-th forward pass on a training plan is the mask of
  * sk_drop with this seed, offset = l * 2^40 + step, and positions image * height * width + pixel of the layer's maps.  sknet_forward on a
  * training plan first adds one to the step, on the device (a recorded pass moves on at every replay), and sknet_backward makes the masks of the
- * pass before it again.  Seed and step start as 0 and outlive plans; set both to repeat or resume a run (step < 2^40).  Both calls synchronise
- * the stream of the last pass. */
+ * pass before it again, whatever was set since.  Seed and step start as 0 and outlive plans; set both to repeat or resume a run (step < 2^40).
+ * A step that is set reaches the replays of a recorded forward pass, a seed does not: the pass keeps the seed it was recorded with, and another
+ * one needs a new recording.  A backward pass goes by the seed of the last sknet_forward call, be that recorded or run.  Both calls synchronise the
+ * stream of the last pass. */
 sk_status sknet_set_dropout(sknet_t *net, uint64_t seed, uint64_t step);
 sk_status sknet_get_dropout(sknet_t *net, uint64_t *seed, uint64_t *step);
 

@@ -108,7 +108,7 @@ template <int DT> __global__ __launch_bounds__(256) void dropout_octets_kernel(D
     }
 }
 
-__global__ void step_add_kernel(uint64_t *step) { *step += 1; }
+__global__ void step_add_kernel(uint64_t *step) { step[1] = step[0] += 1; }
 
 template <int DT> hipError_t launch(const DropoutArgs &a, hipStream_t stream)
 {

@@ -63,7 +63,7 @@ struct NormBwdArgs : NormSpan {
 size_t norm_bwd_scratch_floats(const NormSpan &s);        // of the fastest launch; with less, fewer workgroups share the sums out
 hipError_t launch_layer_norm_bwd(const NormBwdArgs &a, hipStream_t stream);
 
-// *step += 1: one more forward pass (a kernel, so that a recorded pass moves on at every replay)
+// step[0] += 1, one more forward pass, and step[1] = that one's number (a kernel, so that a recorded pass moves on at every replay)
 hipError_t launch_step_add(uint64_t *step, hipStream_t stream);
 
 }  // namespace sk

@@ -66,7 +66,8 @@ struct sknet {
     std::vector<NormParams> norms;
     std::vector<int> norm_of_layer;   // layer -> norm index or -1
     uint64_t drop_seed = 0, drop_step = 0;      // drop_step: while no plan holds the counter
-    uint64_t *step_dev = nullptr;     // training plans of nets with dropout: forward passes so far
+    uint64_t pass_seed = 0;           // of the last forward pass, whose masks the backward pass makes again
+    uint64_t *step_dev = nullptr;     // training plans of nets with dropout: [0] forward passes so far, [1] the number of the last one
     void activate(bool training)
     {
         layers.clear(); user_of.clear(); maps_of.clear(); conv_of_layer.clear(); norm_of_layer.clear();
@@ -222,15 +223,15 @@ void maps_span(const sknet *net, const Dims &d, sk::NormSpan *s)
     s->n = net->n; s->plane = (long)d.h * d.w; s->c = d.c;
 }
 
-// the mask of dropout layer li in the pass that the counter stands at
+// the mask of dropout layer li in the last forward pass
 sk::DropMask layer_mask(const sknet *net, int li)
 {
     sk::DropMask m;
     m.thresh = (uint32_t)net->layers[li].c_out;
     m.scale = m.thresh >= 65536 ? 0.f : (float)(65536.0 / (65536.0 - m.thresh));
-    m.seed = net->drop_seed;
+    m.seed = net->pass_seed;
     m.offset = (uint64_t)net->user_of[li] << 40;
-    m.step = net->step_dev;
+    m.step = net->step_dev + 1;
     return m;
 }
 
@@ -841,7 +842,7 @@ sk_status sknet_plan(sknet_t *net, int32_t n, int32_t h, int32_t w, int32_t pad,
         scratch = std::max(scratch, sk::norm_bwd_scratch_floats(span));
     }
     if (st == SK_OK && training && std::any_of(layers.begin(), layers.end(), [](const sk_layer &l) { return l.kind == SK_DROPOUT; })) {
-        hipError_t e = hipMalloc(reinterpret_cast<void **>(&net->step_dev), sizeof(uint64_t));
+        hipError_t e = hipMalloc(reinterpret_cast<void **>(&net->step_dev), 2 * sizeof(uint64_t));
         st = e == hipSuccess ? put_step(net) : fail(SK_ENOMEM, "plan: hipMalloc of the dropout counter failed: %s", hipGetErrorString(e));
     }
     if (training && net->fuse_head) scratch = std::max(scratch, sk::head_train_scratch_floats(dims[L - 2].c, net->layers[L - 2].c_out));
@@ -897,6 +898,7 @@ sk_status sknet_forward(sknet_t *net, const float *image_dev, float *prob_dev, v
     net->last_image = image_dev;
     net->last_prob = prob_dev;
     net->backward_done = false;
+    net->pass_seed = net->drop_seed;
     if (net->step_dev) SK_HIP(sk::launch_step_add(net->step_dev, stream));      // a mask of its own for every pass
     for (int s = 0; s < (int)net->steps.size(); ++s) SK_TRY(run_forward_step(net, s, stream));
     net->forward_done = true;
