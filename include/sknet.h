@@ -214,7 +214,9 @@ sk_status sknet_sgd_step(sknet_t *net, float lr, float momentum, float weight_de
  * get_activation: output of layer layer_idx (-1 = the padded image) as fp32 NCHW (HOST), sized
  *   as sknet_infer_shapes reports, of the last forward pass: weights set since then change nothing.  Where an fp32
  *   inference plan does not store a layer's maps the layer is run again on its input, with the weights of the pass, into a
- *   temporary that the call allocates and frees (as it does to widen 16-bit maps).
+ *   temporary that the call allocates and frees (as it does to widen 16-bit maps).  SK_ESTATE for what a plan of
+ *   mode 0 or 3 keeps in no other form: the hidden maps and logits of a fused head, and in 16-bit inference pools that run inside their
+ *   neighbours and the padded image where the first layer pads the caller's itself.
  * get_pool_argmax: for max-pool number pool_idx (0-based among pools), per output element the
  *   flat offset (y*W_in + x) of the winning input sample inside its input plane, int32 NCHW
  *   (HOST).  Taps are scanned row-major and only a strictly greater value replaces the
