@@ -138,12 +138,6 @@ __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(N
         float mean[V], rstd[V], sums[2][V] = {};
         t.statistics(a.mean, mean);
         t.statistics(a.rstd, rstd);
-        float once[V], r_once[V];                       // 1 and rstd, 0 where another lane holds the pixel
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            once[v] = t.own(v) ? 1.f : 0.f;
-            r_once[v] = once[v] * rstd[v];
-        }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -152,8 +146,9 @@ __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(N
                 sums[0][v] += g;
                 sums[1][v] += g * d;
                 if (ROLES) continue;
-                dg[j] += y * r_once[v] * d;
-                db[j] += y * once[v];
+                const float mine = t.own(v) ? y : 0.f;  // another lane counts the pixel (a factor of zero would make NaN of an infinite y)
+                dg[j] += mine * rstd[v] * d;
+                db[j] += mine;
             }
         t.template total<2>(sums, part, half);
         if (!a.dx.p && !a.dresidual.p) continue;
