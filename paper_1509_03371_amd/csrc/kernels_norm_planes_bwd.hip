@@ -135,9 +135,16 @@ __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(N
         typename Tile<DT, LAYOUT, P, V>::Octet vy, vs;
         t.load(a.dy, t.oct0, vy);
         t.load(a.s, t.oct0, vs);
+        t.blank(t.oct0, vy);
         float mean[V], rstd[V], sums[2][V] = {};
         t.statistics(a.mean, mean);
         t.statistics(a.rstd, rstd);
+        uint32_t counts[V];                             // zeros where another lane counts the pixel (a factor of zero would make NaN of an infinite y)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            counts[v] = t.own(v) ? ~0u : 0u;
+            asm volatile("" : "+v"(counts[v]));
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(N
                 sums[0][v] += g;
                 sums[1][v] += g * d;
                 if (ROLES) continue;
-                const float mine = t.own(v) ? y : 0.f;  // another lane counts the pixel (a factor of zero would make NaN of an infinite y)
+                const float mine = __uint_as_float(__float_as_uint(y) & counts[v]);
                 dg[j] += mine * rstd[v] * d;
                 db[j] += mine;
             }
@@ -202,6 +209,7 @@ template <int DT, int LAYOUT, int P, int V> __global__ __launch_bounds__(1024) v
         auto take = [&](int o0) {
             t.load(a.dy, o0, vy);
             t.load(a.s, o0, vs);
+            t.blank(o0, vy);
             const int c0 = 8 * (o0 + t.delta);
             octet_values(a.gamma, c0, a.c - c0, 1.f, gamma);
 #pragma unroll

@@ -119,6 +119,21 @@ template <int DT, int LAYOUT, int P, int V> struct Tile {
             for (int v = 0; v < V; ++v) raw.unit[v].load(p, off + 8 * S * behind(v));
         }
     }
+    // zeros for values that stand in for none (repeats of the last channel, of the wave's first octet): a factor of zero would make NaN of infinite ones.
+    // Behind the last channel of OCTETS there are none in memory.
+    __device__ __forceinline__ void blank(int o0, Octet &raw) const
+    {
+        const int left = channels(o0);
+        if (left >= 8) return;
+        if (LAYOUT == MAPS) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j >= left) raw.line[LAYOUT == MAPS ? j : 0].clear();
+        } else if (left <= 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) raw.unit[LAYOUT == MAPS ? 0 : v].clear();
+        }
+    }
     // where line i of an octet that has channels lies: a channel's (MAPS) or a pixel's unit (OCTETS)
     struct Lines {
         dst_t p;

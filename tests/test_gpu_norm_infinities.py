@@ -52,6 +52,17 @@ def test_at_a_pixel_that_two_lanes_hold(shape, kind, adds):
         check(shape, kind, "dense", 3, max(0, shape[2] - back), adds)
 
 
+# the last octet is not whole, or a wave has lanes without one
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("adds", [False, True])
+@pytest.mark.parametrize("shape", [(1, 20, 70001), (2, 40, 40003), (1, 99, 20002), (1, 301, 9001), (1, 776, 5003), (1, 1601, 2001), (1, 20, 901), (1, 40, 901), (2, 2049, 1303),
+                                   (700, 20, 3), (700, 24, 2)], ids=str)
+def test_in_the_last_channels(shape, kind, adds):
+    c = shape[1]
+    for channel in {c - 1, (c - 1) // 8 * 8}:
+        check(shape, kind, "dense", channel, 0, adds)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("adds", [False, True])
 @pytest.mark.parametrize("shape", [(1, 20, 3001), (1, 777, 901), (1, 1000, 37), (2, 5, 700), (1, 20001, 30)], ids=str)
