@@ -16,6 +16,7 @@ PROGRAM = r"""
 
 struct Dim { uint32_t x, y, z; };
 static int launches, failing, last_error, too_large;
+static long groups[8];
 static Dim grid_, block_;
 static size_t lds_;
 static void *stream_;
@@ -24,6 +25,7 @@ int __hipPushCallConfiguration(Dim g, Dim b, size_t lds, void *s) { grid_ = g; b
 int __hipPopCallConfiguration(Dim *g, Dim *b, size_t *lds, void **s) { *g = grid_; *b = block_; *lds = lds_; *s = stream_; return 0; }
 int hipLaunchKernel(const void *, Dim g, Dim b, void **, size_t lds, void *)
 {
+    if (launches < 8) groups[launches] = (long)g.x * g.y;
     ++launches;
     const uint32_t most = 0xffffffffu;                  // threads of a grid along an axis
     if ((uint64_t)g.x * b.x > most || (uint64_t)g.y * b.y > 65535u * 1024u || !g.x || !g.y || !b.x || b.x * b.y * b.z > 1024 || lds > 160 * 1024) ++too_large;
@@ -55,6 +57,8 @@ int main(int argc, char **argv)
                                      in_place ? &v[0] : &v[3], adds ? &v[4] : nullptr, (float *)at(8), (float *)at(9), need ? at(10) : nullptr, need, nullptr);
         if (!failing) made = launches;
         printf("%s%d:%d", failing ? " " : "", failing, (int)s);
+        if (failing) continue;
+        for (int i = 0; i < made; ++i) printf("%s%ld", i ? "," : " groups ", groups[i]);
     }
     printf(" launches %d too large %d\n", made, too_large);
     return 0;
@@ -98,12 +102,12 @@ def test_a_failed_launch_is_reported(program, name, dtype, adds, in_place):
     assert r.returncode == 0, r.stdout + r.stderr
     words = r.stdout.split()
     assert words[0] == "0:0" and "launches %d " % launches in r.stdout, r.stdout
-    assert words[1:1 + launches] == ["%d:5" % (i + 1) for i in range(launches)], r.stdout       # SK_EDEVICE whichever it was
+    assert words[3:3 + launches] == ["%d:5" % (i + 1) for i in range(launches)], r.stdout       # SK_EDEVICE whichever it was
 
 
 EMPTY = {"no rows, the most channels": (ROWS, 0, 1 << 27, 1, 0, 1), "no pixels": (MAPS, 3, 1 << 27, 0, 0, 1), "many rows": (ROWS, 1 << 36, 8, 1, 0, 2),
          "many rows of wide gaps": (ROWS, 1 << 26, 64, 1, 1 << 20, 2), "many images": (MAPS, 1 << 36, 9, 3, 0, 3), "one long plane": (MAPS, 1, 24, 1 << 36, 0, 2),
-         "the most channels of maps": (MAPS, 2, 1 << 27, 3, 0, 3)}
+         "the most channels of maps": (MAPS, 40, 1 << 27, 3, 0, 3)}
 
 
 @pytest.mark.parametrize("name", list(CALLS) + list(EMPTY))
@@ -113,3 +117,10 @@ def test_grids_fit_a_launch(program, name, dtype):
     layout, n, c, plane, stride, launches = {**CALLS, **EMPTY}[name]
     r = program(dtype, layout, n, c, plane, 0, 0, stride)
     assert r.returncode == 0 and "launches %d too large 0" % launches in r.stdout, r.stdout
+
+
+def test_sums_of_small_planes_are_shared_out(program):
+    # planes of two pixels of a million images: waves for the card, not sixteen shares of images
+    r = program(0, MAPS, 1 << 20, 64, 2, 0, 0, 0)
+    assert r.returncode == 0
+    assert int(r.stdout.split("groups ")[1].split()[0].split(",")[0]) >= 1024, r.stdout
