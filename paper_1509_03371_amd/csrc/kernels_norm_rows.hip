@@ -317,12 +317,13 @@ template <int DT, int T> __device__ void norm_rows_sums(const NormBwdArgs &a, in
     __shared__ float sums[W][2][64];
     const Row<DT, 8> r(a.c);                            // eight lanes an octet each, eight rows a wave
     const int wave = uniform(threadIdx.x >> 6);
+    const long to_dy = (long)r.S * r.sub * a.dy.sn, to_s = (long)r.S * r.sub * a.s.sn;     // 64 bits: the rows may be far apart
     float dg[8] = {}, db[8] = {};
     for (long row0 = 8 * wave; row0 < a.n; row0 += 8 * W) {
         if (row0 + r.sub >= a.n) break;
         Words<DT, 8> vy, vs;
-        r.load(r.from(a.dy, row0), r.offset(a.dy), block, vy);
-        r.load(r.from(a.s, row0), r.offset(a.s), block, vs);
+        r.load(r.from(a.dy, row0) + to_dy, 0, block, vy);
+        r.load(r.from(a.s, row0) + to_s, 0, block, vs);
         const float mean = a.mean[row0 + r.sub], rstd = a.rstd[row0 + r.sub];
         r.fit(block, false, vy);
         r.fit(block, false, vs);
@@ -696,7 +697,7 @@ hipError_t launch_norm_rows_bwd(const NormBwdArgs &a, int copies, hipStream_t st
         pick_rows_bwd(a.c, far, [&](auto g, auto k, auto t) {
             const long rounds = (a.n + t() / g() - 1) / (t() / g());
             const int all = (int)std::min<long>(rounds, 256 * 1024 / t());
-            const bool roles = sums && !far && takes_roles(a);
+            const bool roles = sums && takes_roles(a);
             if (roles) {
                 const int walkers = results && !a.in_place() ? all : 0, blocks = walkers + (a.c + 63) / 64;
                 if (adds) norm_rows_bwd_kernel<dt(), g(), k(), t(), true, true><<<blocks, t(), 0, stream>>>(a, walkers);

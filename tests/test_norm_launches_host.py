@@ -124,3 +124,14 @@ def test_sums_of_small_planes_are_shared_out(program):
     r = program(0, MAPS, 1 << 20, 64, 2, 0, 0, 0)
     assert r.returncode == 0
     assert int(r.stdout.split("groups ")[1].split()[0].split(",")[0]) >= 1024, r.stdout
+
+
+@pytest.mark.parametrize("c", [40, 300, 6000])
+def test_rows_far_apart_take_as_many_workgroups(program, c):
+    # few rows, one launch: those with the results, and those with the sums of 64 channels each
+    asked = []
+    for stride in (0, 1 << 24):
+        r = program(0, ROWS, 400, c, 1, 0, 0, stride)
+        assert r.returncode == 0 and "launches 1 " in r.stdout, r.stdout
+        asked.append(int(r.stdout.split("groups ")[1].split()[0]))
+    assert asked[1] >= asked[0] > 1, asked
