@@ -1193,7 +1193,7 @@ sk_status sknet_get_activation(sknet_t *net, int32_t layer_idx, float *nchw_host
     if (!net->forward_done) return fail(SK_ESTATE, "get_activation: no forward pass yet");
     if (layer_idx >= 0) layer_idx = net->maps_of[layer_idx] - 1;      // (a dropout layer that an inference plan leaves out: the layer in front of it)
     if (layer_idx >= 0 && !net->kept(layer_idx))
-        return fail(SK_ESTATE, "get_activation: this plan fuses layer %d with its neighbours; plan with mode 2 to keep every layer", layer_idx);
+        return fail(SK_ESTATE, "get_activation: this plan fuses layer %d with its neighbours; plan with mode 2 to keep every layer", net->user_of[layer_idx]);
     if (layer_idx < 0 && net->image_direct)
         return fail(SK_ESTATE, "get_activation: this plan's first layer pads the image itself; plan with mode 2 to keep the padded one");
     SK_HIP(hipStreamSynchronize(net->last_stream));
