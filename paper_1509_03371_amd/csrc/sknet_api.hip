@@ -1329,7 +1329,7 @@ sk_status sknet_time_backward_step(sknet_t *net, const int32_t *labels_dev, int3
         return fail(SK_EINVAL, "time_backward_step: bad arguments");
     if (!net->planned || !net->training || !net->forward_done) return fail(SK_ESTATE, "time_backward_step: needs a forward pass on a training plan");
     const int L = (int)net->layers.size();
-    if (part == 0 && net->layers[layer_idx].kind != SK_CONV) return fail(SK_EINVAL, "time_backward_step: layer %d has no weights", layer_idx);
+    if (part == 0 && net->layers[layer_idx].kind != SK_CONV) return fail(SK_EINVAL, "time_backward_step: part 0 is a convolution's, and layer %d is none", layer_idx);
     if (part == 1 && layer_idx == 0) return fail(SK_EINVAL, "time_backward_step: layer 0 has no input gradient");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     net->last_stream = stream;

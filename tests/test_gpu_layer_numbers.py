@@ -29,3 +29,20 @@ def test_fused_layers_are_named_by_the_callers_number(dtype):
             refused += 1
     assert refused
     net.close()
+
+
+def test_times_of_a_layer_norm_are_those_of_its_input_gradient():
+    from paper_1509_03371_amd import binding as B
+    layers = [S.conv(9, 3, 1, relu=False), S.norm(relu=True), S.dropout(0.2), S.conv(2, 1, 1, relu=False)]
+    net = B.SKNet(layers, 1, 2)
+    for i, (w, b) in enumerate(zip(*S.he_normal_weights(layers, 1, 5))):
+        net.set_weights(i, w, b)
+    net.plan(1, 20, 30, training=True)
+    net.forward(torch.rand(1, 1, 20, 30, device="cuda"))
+    labels = torch.zeros(1, 20, 30, dtype=torch.int32, device="cuda")
+    for i in (1, 2):
+        with pytest.raises(B.SknetError) as e:
+            net.time_backward_step(labels, i, 0, 2)
+        assert e.value.status_name == "SK_EINVAL" and "convolution" in str(e.value) and "weights" not in str(e.value)
+        assert net.time_backward_step(labels, i, 1, 2) >= 0
+    net.close()
