@@ -143,7 +143,7 @@ __global__ __launch_bounds__(T, T == 1024 ? 4 : 2) void norm_planes_bwd_kernel(N
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             counts[v] = t.own(v) ? ~0u : 0u;
-            asm volatile("" : "+v"(counts[v]));
+            if (T != 1024) asm volatile("" : "+v"(counts[v]));  // a word a pixel; where registers are short the compiler's select by the scalar unit
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
