@@ -89,6 +89,7 @@ constexpr int bwd_pixels(int threads) { return threads == 1024 ? 2 : 4; }
 // 4 x 64 x 388^2 bf16: 236 MB in 60 us, the sums of 512 copies (4.7 us) with it = 3.9 TB/s; planes of 128-byte multiples 43 us + 4.7, these begin at any
 // multiple of 32, and their segments touch a fifth line in four.  What did not help: the next tile's loads in flight (57.5 us for 57.1), 64-pixel
 // segments without a barrier (68), 512-byte segments (68: one workgroup a CU).
+// fp32 of 513 to 2048 channels with residual or dropout spills 19 to 20 registers (1000 x 10001: 200 MB in 98 us); 16 bits of these widths fit (60 us).
 //
 // ROLES, for few pixels: the first `walkers` workgroups leave the sums alone, and each of the others takes them for an octet over all pixels, which are
 // read twice (from the L2): one launch and no workspace.

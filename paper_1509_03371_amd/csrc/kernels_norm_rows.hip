@@ -8,8 +8,8 @@ namespace {
 // A row belongs to G lanes; lane l holds channels 8*(k*G + l) .. + 7 for k < K, the whole row in registers: one read of every input, one write of
 // every output, and the variance from the values themselves about their mean (no sum of squares to cancel).  Eight channels a lane because that is
 // what one call of dropout's generator serves; 16 bytes a load in 16 bits, two loads in fp32.  Rows of up to 64 lanes' worth need no LDS; longer ones
-// add their waves' sums there.  HBM bounds it: 65536 x 2048 bf16 537 MB in 105 us = 5.1 TB/s, with residual, dropout and sum 16384 x 4096 bf16 537 MB in 95 us =
-// 5.7 TB/s (a copy of 256 MB: 5.3); the first kernel, which read each row three times, took 544 and 605 us.
+// add their waves' sums there.  HBM bounds it: 65536 x 2048 bf16 537 MB in 103.5 us = 5.2 TB/s, with residual, dropout and sum 16384 x 4096 bf16 537 MB in 94 us =
+// 5.7 TB/s (copies of 512 MB: 5.1 to 5.3; under a trace 107 to 112 and 95); the first kernel, which read each row three times, took 544 and 605 us.
 template <int DT, int G> struct Row {
     typedef elem_t<DT> E;
     static constexpr int S = sizeof(E);
@@ -307,7 +307,9 @@ __device__ __forceinline__ void put_values(float *out, int c, int c0, const floa
 // Backwards: a workgroup takes R = T / G rows at a time, gridDim.x * R apart, and keeps its lanes' sums for dgamma and dbeta in registers until the end,
 // where they are added up over the R rows' lanes through LDS and go to the workgroup's copy [2][c rounded up to 4] of the scratch, or to dgamma and dbeta
 // themselves if there is one workgroup.  Eight waves a workgroup: with four, twice the copies, whose writing and adding up made 147 us of 134 for
-// 16384 x 4096 bf16 with dropout and residual (671 MB: 5.1 TB/s).  Few rows a wave are bound by latency: 8192 x 1001 fp16, two rows a wave, 15.3 us for 49 MB.
+// 16384 x 4096 bf16 with dropout and residual (671 MB: 5.1 TB/s).  Few rows a wave are bound by latency: 8192 x 1001 fp16, two rows a wave, 15 us for 49 MB.
+// With residual or dropout 513 to 1024 channels spill registers (43 in fp32, 13 in 16 bits; wider fp32 rows 16 to 20): 16384 x 1024 fp32 336 MB in 83 us = 4.0
+// TB/s, bf16 168 MB in 43 = 3.9.
 //
 // ROLES, for few rows: the first `walkers` workgroups leave the sums alone, and each of the others takes them for 64 channels over all rows, which are read twice
 // (from the L2): one launch and no workspace.

@@ -6,7 +6,7 @@ import torch
 from norm_bounds import bwd_bounds, close, inputs, place, rounded, to64
 from oracle import norm as ON
 
-pytestmark = pytest.mark.gpu
+pytestmark = [pytest.mark.gpu, pytest.mark.filterwarnings("ignore:invalid value encountered")]          # (infinite less infinite)
 
 
 def check(shape, kind, order, channel, pixel, adds):
