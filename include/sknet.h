@@ -406,13 +406,15 @@ sk_status sknet3d_get_pool_argmax(sknet3d_t *net, int32_t pool_idx, int32_t *idx
  *   SK_ROWS: channel k of row r is element r*stride_n + k; plane must be 1 and stride_c is ignored;
  *   SK_MAPS: channel k of pixel m of image b is element b*stride_n + k*stride_c + m (planes of pixels, as the maps of a net).
  * Position number: b*plane + m.  Strides count elements and may be larger than a dense tensor's; inputs may have strides of 0,
- * of an output the images must lie one behind the other or the maps must (SK_ESHAPE), so that no two elements share a place.  dtype is the type of every sk_view of a call; parameters, statistics and
+ * of an output the images must lie one behind the other or the maps must (SK_ESHAPE), so that no two elements share a place.
+ * dtype is the type of every sk_view of a call; parameters, statistics and
  * parameter gradients are fp32, and so is everything in between: 16-bit values are rounded when they are stored, once.
  * Data need no alignment beyond their elements'.  n or plane of 0 is allowed (the views' data may then be NULL): nothing runs but the clearing of
  * parameter gradients.  Limits (SK_EUNSUPPORTED): 2^27 channels, 2^40 positions, 2^46 elements reached.
  *
  * In place: an output may be the tensor of an input, with the same strides.  SK_EINVAL for any other overlap of an output
- * with an input or another output, as far as views of one call go (views of equal strides by their elements, others by their ranges of memory); the fp32 values that a call writes, and its workspace, must
+ * with an input or another output, as far as views of one call go (views of equal strides by their elements, others by their
+ * ranges of memory); the fp32 values that a call writes, and its workspace, must
  * not overlap other fp32 values of the call (SK_EINVAL), nor its views.
  *
  * Everything is enqueued on hip_stream; the current HIP device must be that of the stream and the buffers.  Nothing is
