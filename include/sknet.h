@@ -467,6 +467,63 @@ sk_status sknet_layer_norm_backward(const sk_extent *extent, const sk_view *dy, 
                                     const float *gamma_dev, const sk_view *dsum, const sk_drop *drop, const sk_view *dx, const sk_view *dresidual,
                                     float *dgamma_dev, float *dbeta_dev, void *workspace_dev, uint64_t workspace_bytes, void *hip_stream);
 
+/* ---- Activations in 8 bits, and root-mean-square norm
+ *
+ * A tensor in 8 bits: each line (SK_ROWS: the c channels of a row; SK_MAPS: the plane pixels of a map) is cut into blocks of 32 neighbours from its
+ * first element on; the last may be shorter.  A block has a scale 2^k, kept as the byte k + 127: k is the least integer of at least -117 for which the
+ * block's largest magnitude is at most Q 2^k.  A code is value / 2^k rounded to the nearest, ties to even:
+ *   SK_E4M3: Q = 448; sign, 4 bits of exponent (bias 7), 3 of mantissa, no infinities, 0x7F (and 0xFF) = NaN;
+ *   SK_I8  : Q = 127; two's complement of -127 .. 127, -128 = NaN.
+ * So a value is off by at most half a step: SK_E4M3 2^-4 of itself or 2^(k-10) (values below 2^(k-6)), SK_I8 2^(k-1) < largest / 126.  Infinite and NaN elements
+ * become NaN and leave the others of their block as they are: the largest is taken over the finite ones.  Magnitudes beyond the largest that
+ * a code can stand for in the extent's dtype are limited to it (SK_F16: 61440 and 65024, else 1.875 * 2^127 and 127 * 2^121), so that finite values stay finite.
+ * What a code stands for is exact in bf16.
+ *
+ * codes: element (position, channel) is the byte at the place that an sk_view of these strides gives it.  scales: of the line of row b, or of map k
+ * of image b, at b*scale_stride_n (+ k*scale_stride_c), one byte for each block, side by side.  Lines of a result must not overlap (SK_ESHAPE).  scales
+ * that sknet_unpack8 or another call reads may hold any byte 10 .. 248; other scales, which no call here writes, give unspecified values.
+ *
+ * Extents, views, in-place results, streams and graphs as above; results (codes and scales, fp32 values and the workspace among them) must not
+ * overlap anything else of the call (SK_EINVAL) but where a view may be another's place.  Operands of equal strides in bytes are compared line by
+ * line, others by their ranges of memory. */
+typedef enum { SK_E4M3 = 0, SK_I8 = 1 } sk_code;
+typedef struct {
+    int32_t code;             /* sk_code */
+    uint8_t *codes, *scales;  /* DEVICE */
+    int64_t stride_n, stride_c;
+    int64_t scale_stride_n, scale_stride_c;
+} sk_packed;
+
+/* packed = x in 8 bits;  y = what packed stands for, rounded to the extent's dtype (exact but in SK_F16). */
+sk_status sknet_pack8(const sk_extent *extent, const sk_view *x, const sk_packed *packed, void *hip_stream);
+sk_status sknet_unpack8(const sk_extent *extent, const sk_packed *packed, const sk_view *y, void *hip_stream);
+
+/* s = x + residual (residual: NULL leaves it out);  per position: rstd = 1 / sqrt(sum_k s^2 / c + eps);  y = s * rstd * gamma.
+ * gamma_dev: DEVICE [c], NULL = 1.  Results, each may be NULL: sum and sum8 receive s, y and y8 receive y, in the extent's type and in 8 bits, all made from the
+ * fp32 values, rounded once; rstd_dev: DEVICE [n*plane].  y or sum may be x or residual.  eps > 0. */
+sk_status sknet_rms_norm(const sk_extent *extent, const sk_view *x, const sk_view *residual, const float *gamma_dev, float eps, const sk_view *sum,
+                         const sk_packed *sum8, const sk_view *y, const sk_packed *y8, float *rstd_dev, void *hip_stream);
+
+/* Gradients of sknet_rms_norm.  What was normalised is s (a view) or s8 (held in 8 bits): one of the two.  With h = s * rstd and g = gamma * dy:
+ *   dx = rstd * (g - h * sum_k(g h) / c) + dsum, the gradient of x and of the residual alike;  dgamma = sum over positions of dy h.
+ * dsum: the gradient that reaches s from elsewhere, or NULL.  dx (which may be dy, s or dsum) and dgamma_dev: each may be NULL.  Equal calls give equal bits.
+ * workspace_dev: DEVICE, 16-byte aligned, of at least the bytes that sknet_rms_norm_workspace reports, used until the call's work has run (NULL where
+ * that is 0, or without dgamma). */
+sk_status sknet_rms_norm_workspace(const sk_extent *extent, uint64_t *bytes);
+sk_status sknet_rms_norm_backward(const sk_extent *extent, const sk_view *dy, const sk_view *s, const sk_packed *s8, const float *rstd_dev,
+                                  const float *gamma_dev, const sk_view *dsum, const sk_view *dx, float *dgamma_dev, void *workspace_dev,
+                                  uint64_t workspace_bytes, void *hip_stream);
+
+/* Weight gradient of an inner product, or of a 1x1 convolution, over inputs held in 8 bits: with the extent's n * plane positions q and c input channels k,
+ *   dw[o][k] = sum_q dy[q][o] x[q][k],  db[o] = sum_q dy[q][o]      (accumulate != 0: added to what dw and db hold)
+ * dy: of the extent's type and order with c_out channels in the place of c.  dw_dev: DEVICE [c_out][c], db_dev: DEVICE [c_out] or NULL.  Products are exact:
+ * dy goes to the matrix unit whole (bf16) or as two (fp16) or three (fp32) bf16 terms that add up to it, x as it is; sums are fp32, in an order
+ * that the sizes alone settle: equal calls give equal bits.  workspace_dev as above, from sknet_weight_gradient8_workspace.
+ * Limits (SK_EUNSUPPORTED): those of an extent, c_out <= 2^27, c * c_out <= 2^40. */
+sk_status sknet_weight_gradient8_workspace(const sk_extent *extent, int64_t c_out, uint64_t *bytes);
+sk_status sknet_weight_gradient8(const sk_extent *extent, int64_t c_out, const sk_view *dy, const sk_packed *x, int32_t accumulate, float *dw_dev,
+                                 float *db_dev, void *workspace_dev, uint64_t workspace_bytes, void *hip_stream);
+
 /* Machine probes for the benchmark (Section 6 of the paper times kernels against each device's
  * peak; these two calls measure the peaks of the device at hand).  Neither runs any step of the method.
  *

@@ -3,8 +3,10 @@ only.  Device buffers are torch CUDA tensors (used for memory and streams, nothi
 step of the path runs inside the library's HIP kernels.  There is no CPU fallback: if the library
 is missing, importing this module raises.
 """
+import contextlib
 import ctypes as C
 import functools
+import math
 import os
 
 import numpy as np
@@ -20,8 +22,10 @@ lib = C.CDLL(LIB_PATH)
 SK_F32, SK_BF16, SK_F16 = 0, 1, 2
 SK_CONV, SK_MAXPOOL, SK_LAYERNORM, SK_DROPOUT = 0, 1, 2, 3
 SK_ROWS, SK_MAPS = 0, 1
+SK_E4M3, SK_I8 = 0, 1
 STATUS_NAMES = ["SK_OK", "SK_EINVAL", "SK_ESHAPE", "SK_ESTATE", "SK_ENOMEM", "SK_EDEVICE", "SK_EUNSUPPORTED"]
 DTYPES = {"f32": SK_F32, "bf16": SK_BF16, "f16": SK_F16}
+CODES = {"e4m3": SK_E4M3, "i8": SK_I8}
 
 
 class SkLayer(C.Structure):
@@ -44,6 +48,11 @@ class SkView(C.Structure):
 
 class SkDrop(C.Structure):
     _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64), ("step_dev", C.c_void_p)]
+
+
+class SkPacked(C.Structure):
+    _fields_ = [("code", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p), ("stride_n", C.c_int64), ("stride_c", C.c_int64),
+                ("scale_stride_n", C.c_int64), ("scale_stride_c", C.c_int64)]
 
 
 class SknetError(RuntimeError):
@@ -118,6 +127,13 @@ _SIGS = {
     "sknet_layer_norm": [_vp, _vp, _vp, _vp, _vp, _vp, C.c_float, _vp, _vp, _vp, _vp, _vp],
     "sknet_layer_norm_workspace": [_vp, C.POINTER(C.c_uint64)],
     "sknet_layer_norm_backward": [_vp] * 13 + [C.c_uint64, _vp],
+    "sknet_pack8": [_vp] * 4,
+    "sknet_unpack8": [_vp] * 4,
+    "sknet_rms_norm": [_vp] * 4 + [C.c_float] + [_vp] * 6,
+    "sknet_rms_norm_workspace": [_vp, C.POINTER(C.c_uint64)],
+    "sknet_rms_norm_backward": [_vp] * 10 + [C.c_uint64, _vp],
+    "sknet_weight_gradient8_workspace": [_vp, C.c_int64, C.POINTER(C.c_uint64)],
+    "sknet_weight_gradient8": [_vp, C.c_int64, _vp, _vp, _i32] + [_vp] * 3 + [C.c_uint64, _vp],
     "sk_probe_mfma": [_i32, _i32, _i32, _vp, C.POINTER(C.c_double)],
     "sk_probe_copy": [_vp, _vp, C.c_uint64, _i32, _vp, C.POINTER(C.c_double)],
     "sk_probe_conv_path": [_i32] * 8 + [_ip],
@@ -318,14 +334,16 @@ class _Operator:
         if self.scope is not None:
             self.scope.__exit__(*exc)
 
-    def output(self):
+    def output(self, dtype=None):
         """A tensor for a result: x's sizes and order of axes, without its gaps."""
-        return torch.empty_like(self.x, memory_format=torch.contiguous_format if self.x.is_contiguous() else torch.preserve_format)
+        return torch.empty_like(self.x, dtype=dtype, memory_format=torch.contiguous_format if self.x.is_contiguous() else torch.preserve_format)
 
-    def place(self, **tensors):
-        """Find the order that the tensors have in common; returns the extent, and their views by name (None for None)."""
+    def place(self, order=None, **tensors):
+        """Find the order that the tensors have in common (order: that one alone); returns the extent, and their views by name (None for None)."""
         x, axis = self.x, self.axis
         choices = _orders(x.shape, x.stride(), axis)
+        if order is not None:
+            choices = {o: strides for o, strides in choices.items() if o == order}
         theirs = {}
         for name, t in tensors.items():
             if t is None or t is x:
@@ -433,6 +451,195 @@ def layer_norm_backward(dy, s, mean, rstd, gamma=None, axis=-1, dsum=None, p=0.0
                                              op.values(gamma, c, "gamma"), dsv, drop, dxv, drv, op.values(dgamma, c, "dgamma"),
                                              op.values(dbeta, c, "dbeta"), None if workspace is None else workspace.data_ptr(), bytes_, op.stream))
     return dx, dx if p == 0.0 else dresidual, dgamma, dbeta
+
+
+class Packed:
+    """A tensor in 8 bits, in blocks of 32 neighbours with a scale each.  codes: uint8 tensor of the tensor's sizes, with the channels on `axis`, as
+    rows or as maps; scales: uint8 tensor of [positions, blocks of a row] or [images, channels, blocks of a map], which tells the two apart.
+    code: "e4m3" or "i8"."""
+
+    def __init__(self, codes, scales, code="e4m3", axis=-1):
+        for t, name in ((codes, "codes"), (scales, "scales")):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.uint8):
+                raise TypeError("%s must be a CUDA tensor of torch.uint8" % name)
+        if scales.device != codes.device:
+            raise TypeError("scales must be on %s" % (codes.device,))
+        if code not in CODES:
+            raise ValueError("code must be one of %s" % sorted(CODES))
+        if not -codes.dim() <= axis < codes.dim():
+            raise ValueError("codes has no axis %d" % axis)
+        self.codes, self.scales, self.code, self.axis = codes, scales, code, axis % codes.dim()
+        self.order, strides = _packed_order(codes.shape, codes.stride(), self.axis, scales.shape, scales.stride())
+        self.view = SkPacked(CODES[code], codes.data_ptr(), scales.data_ptr(), *strides)
+
+    @classmethod
+    def like(cls, x, code="e4m3", axis=-1):
+        """Room for x in 8 bits, without x's gaps."""
+        with _Operator(x, axis, "x", None) as op:
+            choices = _orders(x.shape, x.stride(), op.axis)
+            if not choices:
+                raise ValueError("x, strides %s, keeps the channels of axis %d neither as rows nor as maps; make it contiguous" % (x.stride(), op.axis))
+            # rows where the channels lie behind everything else; else the axes in front of them are images and those behind them pixels
+            images, pixels = math.prod(x.shape[:op.axis]), math.prod(x.shape[op.axis + 1:])
+            natural = (SK_MAPS, images, x.shape[op.axis], pixels)
+            layout, n, c, plane = natural if pixels > 1 and natural in choices else next(iter(choices))
+            codes = op.output(torch.uint8)
+            blocks = ((c if layout == SK_ROWS else plane) + 31) // 32
+            return cls(codes, torch.empty((n, blocks) if layout == SK_ROWS else (n, c, blocks), dtype=torch.uint8, device=x.device), code, op.axis)
+
+
+@functools.lru_cache(maxsize=4096)
+def _packed_order(shape, strides, axis, scales_shape, scales_strides):
+    """The order of codes that goes with scales of these sizes, and the strides of both."""
+    found = _orders(shape, strides, axis)
+    for (layout, n, c, plane), (stride_n, stride_c) in found.items():
+        blocks = ((c if layout == SK_ROWS else plane) + 31) // 32
+        if n == 0:
+            return (layout, n, c, plane), (0, 0, 0, 0)
+        if scales_shape != ((n, blocks) if layout == SK_ROWS else (n, c, blocks)) or (blocks > 1 and scales_strides[-1] != 1):
+            continue
+        return (layout, n, c, plane), (stride_n, stride_c, scales_strides[0], 0 if layout == SK_ROWS else scales_strides[1])
+    raise ValueError("codes of %s, strides %s, channels on axis %d, and scales of %s, strides %s: [positions, ceil(c / 32)] of rows or [images, c, ceil(pixels / 32)] of "
+                     "maps, blocks side by side, is wanted" % (tuple(shape), strides, axis, tuple(scales_shape), scales_strides))
+
+
+def _packed(op, p, name):
+    """Reference to a Packed of the operator's sizes, None for None."""
+    if p is None:
+        return None
+    if not isinstance(p, Packed):
+        raise TypeError("%s must be a Packed" % name)
+    if p.codes.device != op.device:
+        raise TypeError("%s must be on %s" % (name, op.device))
+    if p.codes.shape != op.x.shape or p.axis != op.axis:
+        raise ValueError("%s has shape %s and channels on axis %d instead of %s and %d" % (name, tuple(p.codes.shape), p.axis, tuple(op.x.shape), op.axis))
+    return C.byref(p.view)
+
+
+def _one_order(*packed):
+    """The order of those that are there; theirs have to agree."""
+    orders = {p.order for p in packed if isinstance(p, Packed)}
+    if len(orders) > 1:
+        raise ValueError("the tensors in 8 bits are in unlike orders: %s" % sorted(orders))
+    return orders.pop() if orders else None
+
+
+def pack8(x, code="e4m3", axis=-1, out=None, stream=None):
+    """x in 8 bits: a Packed (out: one to write to, whose code counts)."""
+    with _Operator(x, axis, "x", stream) as op:
+        if out is None:
+            out = Packed.like(x, code, axis)
+        packed = _packed(op, out, "out")
+        xv, = op.place(out.order)
+        _check(lib.sknet_pack8(C.byref(op.extent), xv, packed, op.stream))
+    return out
+
+
+def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
+    """What a Packed stands for, as a tensor of dtype (out: one to write to)."""
+    if not isinstance(packed, Packed):
+        raise TypeError("packed must be a Packed")
+    if out is None:
+        device = packed.codes.device
+        if dtype not in _OP_TYPES:
+            raise TypeError("dtype must be one of %s" % sorted(map(str, _OP_TYPES)))
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=device)
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            out = torch.empty_like(packed.codes, dtype=dtype)
+    with _Operator(out, packed.axis, "out", stream) as op:
+        ref = _packed(op, packed, "packed")
+        yv, = op.place(packed.order)
+        _check(lib.sknet_unpack8(C.byref(op.extent), ref, yv, op.stream))
+    return out
+
+
+def rms_norm(x, gamma=None, eps=1e-5, axis=-1, residual=None, out=None, sum_out=None, rstd=None, y8=None, sum8=None, stream=None):
+    """(y, s, rstd): y = s * rstd * gamma with s = x + residual and rstd = 1 / sqrt(mean of s^2 + eps) over the channels on `axis`.  s is x itself without a
+    residual; rstd has x's axes without the channels'.  out, sum_out, rstd: tensors to write to; out=False: no y, sum_out=False: no s (None).  y8, sum8:
+    Packed that receive y and s in 8 bits (Packed.like makes one)."""
+    with _Operator(x, axis, "x", stream) as op:
+        if out is None:
+            out = op.output()
+        if sum_out is None and residual is not None:
+            sum_out = op.output()
+        if rstd is None:
+            rstd = torch.empty(x.shape[:op.axis] + x.shape[op.axis + 1:], dtype=torch.float32, device=x.device)
+        packed = _packed(op, sum8, "sum8"), _packed(op, y8, "y8")
+        xv, rv, sv, yv = op.place(_one_order(sum8, y8), residual=residual, sum_out=None if sum_out is False else sum_out, out=None if out is False else out)
+        _, n, c, plane = op.order
+        _check(lib.sknet_rms_norm(C.byref(op.extent), xv, rv, op.values(gamma, c, "gamma"), eps, sv, packed[0], yv, packed[1],
+                                  op.values(rstd, n * plane, "rstd"), op.stream))
+    return None if out is False else out, None if sum_out is False else x if sum_out is None else sum_out, rstd
+
+
+@functools.lru_cache(maxsize=4096)
+def _rms_workspace(dtype, layout, n, c, plane):
+    need = C.c_uint64()
+    _check(lib.sknet_rms_norm_workspace(C.byref(SkExtent(dtype, layout, n, c, plane)), C.byref(need)))
+    return need.value
+
+
+def rms_norm_backward(dy, s, rstd, gamma=None, axis=-1, dsum=None, parameters=True, dx=None, dgamma=None, stream=None):
+    """(dx, dgamma) of rms_norm's y, with its rstd and what it normalised: s, a tensor or a Packed.  dsum: the gradient that reaches s from elsewhere.  dx is
+    the gradient of x and of the residual alike.  parameters=False: no dgamma (None)."""
+    with _Operator(dy, axis, "dy", stream) as op:
+        if dx is None:
+            dx = op.output()
+        held = s if isinstance(s, Packed) else None
+        ref = _packed(op, held, "s")
+        dyv, sv, dsv, dxv = op.place(_one_order(held), s=None if held else s, dsum=dsum, dx=dx)
+        _, n, c, plane = op.order
+        workspace, bytes_ = None, 0
+        if parameters:
+            dgamma = torch.empty(c, dtype=torch.float32, device=dy.device) if dgamma is None else dgamma
+            bytes_ = _rms_workspace(op.extent.dtype, *op.order)
+            if bytes_:
+                workspace = torch.empty(bytes_, dtype=torch.uint8, device=dy.device)
+        elif dgamma is not None:
+            raise ValueError("parameters=False leaves no gradient to write")
+        _check(lib.sknet_rms_norm_backward(C.byref(op.extent), dyv, sv, ref, op.values(rstd, n * plane, "rstd"), op.values(gamma, c, "gamma"), dsv, dxv,
+                                           op.values(dgamma, c, "dgamma"), None if workspace is None else workspace.data_ptr(), bytes_, op.stream))
+    return dx, dgamma
+
+
+@functools.lru_cache(maxsize=4096)
+def _gradient8_workspace(dtype, layout, n, c, plane, c_out):
+    need = C.c_uint64()
+    _check(lib.sknet_weight_gradient8_workspace(C.byref(SkExtent(dtype, layout, n, c, plane)), c_out, C.byref(need)))
+    return need.value
+
+
+def weight_gradient8(dy, x, accumulate=False, bias=True, dw=None, db=None, stream=None):
+    """(dw, db) of an inner product or 1x1 convolution y = W x + b from the gradient dy of y and its input held in 8 bits, a Packed: dw[o, k] = sum over
+    positions of dy[o] x[k], db[o] = sum of dy[o].  dy has x's axes with the outputs in the channels' place.  accumulate: added to what dw and db
+    hold (give both).  bias=False: no db (None)."""
+    if not isinstance(x, Packed):
+        raise TypeError("x must be a Packed")
+    with _Operator(dy, x.axis, "dy", stream) as op:
+        if x.codes.device != op.device:
+            raise TypeError("x must be on %s" % (op.device,))
+        layout, n, c, plane = x.order
+        c_out = dy.shape[op.axis] if dy.dim() == x.codes.dim() else -1
+        if dy.shape != x.codes.shape[:x.axis] + (c_out,) + x.codes.shape[x.axis + 1:]:
+            raise ValueError("dy has shape %s, x %s with channels on axis %d" % (tuple(dy.shape), tuple(x.codes.shape), x.axis))
+        if accumulate and (dw is None or (bias and db is None)):
+            raise ValueError("accumulate needs the dw and db to add to")
+        if not bias and db is not None:
+            raise ValueError("bias=False leaves no gradient to write")
+        dyv, = op.place((layout, n, c_out, plane))
+        extent = SkExtent(op.extent.dtype, layout, n, c, plane)
+        if dw is None:
+            dw = torch.empty((c_out, c), dtype=torch.float32, device=op.device)
+        elif tuple(dw.shape) != (c_out, c):
+            raise ValueError("dw has shape %s instead of %s" % (tuple(dw.shape), (c_out, c)))
+        if db is None and bias:
+            db = torch.empty(c_out, dtype=torch.float32, device=op.device)
+        bytes_ = _gradient8_workspace(extent.dtype, layout, n, c, plane, c_out)
+        workspace = torch.empty(bytes_, dtype=torch.uint8, device=op.device) if bytes_ else None
+        _check(lib.sknet_weight_gradient8(C.byref(extent), c_out, dyv, C.byref(x.view), int(accumulate), op.values(dw, c_out * c, "dw"),
+                                          op.values(db, c_out, "db"), None if workspace is None else workspace.data_ptr(), bytes_, op.stream))
+    return dw, db
 
 
 class SKNet:
