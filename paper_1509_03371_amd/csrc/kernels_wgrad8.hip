@@ -1,52 +1,378 @@
-// Weight gradient of an inner product over inputs held in 8 bits.
+// Weight gradient of an inner product over inputs held in 8 bits: dw[o][k] = sum over positions q of dy[q][o] x[q][k].
 #include "act8_device.h"
+#include "reduce_copies.h"
 
 namespace sk {
 
 namespace {
 
-// a thread an element of the gradient
-template <int DT, int CODE> __global__ __launch_bounds__(256) void wgrad8_kernel(Wgrad8Args a)
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+// What a code stands for is exact in bf16, and so x goes to the matrix unit; dy goes there as bf16 terms that add up to it.  fp16 has 11 bits, two terms of
+// 8; fp32 24, three.  Each term is cut off, not rounded, so what is left is exact and no term overflows; an infinite value has no rest.
+template <int DT> constexpr int terms = DT == 1 ? 1 : DT == 2 ? 2 : 3;
+
+constexpr int KS = 64;                                  // positions of a step: two blocks of a map's line, or rows
+constexpr int MAPS_PITCH = 2 * KS + 16;                 // bytes from one channel to the next in LDS
+constexpr int T = 256;
+
+struct Plan8 {
+    int tm, tn;                                         // output and input channels of a workgroup's tile
+    long tiles_m, tiles_n, steps, splits;
+};
+
+// As many workgroups as fill the card twice, so long as each takes four steps or more; tiles of 64 where those of 128 would be half empty or too few.
+Plan8 plan_of(const NormSpan &s, long c_out)
 {
-    const bool rows = a.layout == ROWS;
-    const long all = a.c_out * (a.c + (a.db ? 1L : 0L));
-    for (long i = blockIdx.x * 256L + threadIdx.x; i < all; i += gridDim.x * 256L) {
-        const bool bias = i >= a.c_out * a.c;
-        const long o = bias ? i - a.c_out * a.c : i / a.c, k = bias ? 0 : i - o * a.c;
-        const long positions = a.n * a.plane;
-        float sum = 0.f;
-        for (long q0 = 0; q0 < positions; q0 += 32) {
-            float part = 0.f;
-            for (long q = q0; q < q0 + 32 && q < positions; ++q) {
-                const long b = q / a.plane, m = q - b * a.plane;
-                const float dy = (float)static_cast<const elem_t<DT> *>(a.dy.p)[b * a.dy.sn + (rows ? o : o * a.dy.sc + m)];
-                if (bias) {
-                    part += dy;
+    Plan8 p;
+    p.steps = s.layout == ROWS ? (s.n + KS - 1) / KS : s.n * ((s.plane + KS - 1) / KS);
+    const long most = std::max<long>(1, p.steps / 4);
+    auto count = [&](int tm, int tn) { return ((c_out + tm - 1) / tm) * ((s.c + tn - 1) / tn); };
+    p.tm = c_out <= 64 ? 64 : 128;
+    p.tn = s.c <= 64 ? 64 : 128;
+    if (count(p.tm, p.tn) * most < 256) p.tm = p.tn = 64;
+    p.tiles_m = (c_out + p.tm - 1) / p.tm;
+    p.tiles_n = (s.c + p.tn - 1) / p.tn;
+    const long tiles = p.tiles_m * p.tiles_n;
+    p.splits = std::min(most, std::max<long>(1, 512 / tiles));
+    return p;
+}
+long copy_floats(const NormSpan &s, long c_out) { return (c_out * (s.c + 1) + 3) / 4 * 4; }
+
+struct Wgrad8Launch : Wgrad8Args {
+    long tiles_n, tiles, steps, splits, plane_steps, copy;
+    long dy_end, codes_end;                             // bytes that the operands span
+    float *to;                                          // dw, or the copies of it
+};
+
+// 32 values of a line: codes or dy, as read
+template <int B> struct Unit {                          // B bytes a value
+    uint32_t w[8 * B];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 8 * B; ++i) w[i] = 0;
+    }
+    // `count` values at `off` of an operand that spans `end` bytes.  Whole vectors where the operand goes on for as long; what they bring behind `count` is
+    // some other value of it.
+    __device__ __forceinline__ void load(const char *base, long off, long end, int count)
+    {
+        if (off + 32 * B <= end) {
+            typedef uint32_t Four __attribute__((ext_vector_type(4), aligned(1)));
+#pragma unroll
+            for (int i = 0; i < 2 * B; ++i) {
+                const Four v = reinterpret_cast<const Four *>(base + off)[i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+            }
+        } else {
+            clear();
+#pragma unroll 1
+            for (int j = 0; j < count; ++j) {           // (the operand's last values: a short loop, not many registers)
+                const char *p = base + off + B * j;
+                const uint32_t v = B == 1 ? *reinterpret_cast<const uint8_t *>(p) : B == 2 ? *reinterpret_cast<const uint16_t *>(p) : *reinterpret_cast<const uint32_t *>(p);
+#pragma unroll
+                for (int i = 0; i < 8 * B; ++i) w[i] |= i == B * j / 4 ? v << 8 * (B * j % 4) : 0;
+            }
+        }
+    }
+    // zeros behind `count`: positions that are not there must not reach the sums
+    __device__ __forceinline__ void keep(int count)
+    {
+#pragma unroll
+        for (int i = 0; i < 8 * B; ++i) {
+            const int left = (count * B - 4 * i) * 8;
+            w[i] = left >= 32 ? w[i] : left <= 0 ? 0 : w[i] & ((1u << left) - 1);
+        }
+    }
+};
+
+template <int CODE> __device__ __forceinline__ void widen(const Unit<1> &u, float scale, words4 (&to)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (CODE == E4M3) {
+            to[i / 2][2 * (i % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u.w[i], scale, false));
+            to[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u.w[i], scale, true));
+        } else {
+            float f[4];
+            Code8<CODE>::values(u.w[i], scale, f);
+            // exact: the upper halves are the values
+            to[i / 2][2 * (i % 2)] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302);
+            to[i / 2][2 * (i % 2) + 1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302);
+        }
+    }
+}
+
+__device__ __forceinline__ float rest(float v) { return magnitude(v) == 0x7f800000u ? 0.f : v - __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+
+// term n of the unit's values
+template <int DT> __device__ __forceinline__ void term(Unit<DT == 0 ? 4 : 2> &u, int n, words4 (&to)[4])
+{
+    if constexpr (DT == 1) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[i / 4][i % 4] = u.w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float a, b;
+            if constexpr (DT == 2) {
+                a = (float)__builtin_bit_cast(_Float16, (uint16_t)u.w[i]);
+                b = (float)__builtin_bit_cast(_Float16, (uint16_t)(u.w[i] >> 16));
+                if (n == 1) {
+                    a = rest(a);
+                    b = rest(b);
+                }
+            } else {
+                a = __uint_as_float(u.w[2 * i]);
+                b = __uint_as_float(u.w[2 * i + 1]);
+                u.w[2 * i] = __float_as_uint(rest(a));              // for the next term
+                u.w[2 * i + 1] = __float_as_uint(rest(b));
+            }
+            to[i / 4][i % 4] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+        }
+    }
+}
+
+// Lane l of a fragment holds channel l % 16 at eight of 32 positions; which eight is the same for both operands, and that is all that matters.  MAPS keep a channel's
+// positions side by side in LDS.  ROWS keep a position's channels side by side, and a transposing read makes of four positions' sixteen channels
+// (lane 4 r + p of sixteen names position r, channels 4 p ..) each channel's four positions: those at 4 g .. and at 16 + 4 g .. for group g of sixteen lanes, which
+// lie in as many banks as there are.
+template <bool IS_ROWS> __device__ __forceinline__ bf16x8 fragment(const char *lds, int pitch, int channel, int position)
+{
+    const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+    if constexpr (IS_ROWS) {
+        typedef shortx4 __attribute__((address_space(3))) *lds_s4;
+        const char *at = lds + (position + 4 * g + (l >> 2)) * pitch + 2 * channel + 8 * (l & 3);
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)at);
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + 16 * pitch));
+        typedef short shortx8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(bf16x8, shortx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    } else {
+        return *reinterpret_cast<const bf16x8 *>(lds + (channel + l) * pitch + 2 * position + 16 * g);
+    }
+}
+
+// A workgroup takes TM x TN weights and a share of the positions, KS at a time: its threads load 32 values of a line each (of x a block with its scale), one step
+// ahead, widen them on their way into LDS, and four waves multiply, a quarter of the tile each.  db comes out of the same fragments, times ones.
+template <int DT, int CODE, bool IS_ROWS, int TM, int TN> __global__ __launch_bounds__(T) void wgrad8_kernel(Wgrad8Launch a)
+{
+    constexpr int NS = terms<DT>, B = DT == 0 ? 4 : 2;
+    constexpr int pitch_m = IS_ROWS ? 2 * TM + 32 : MAPS_PITCH, pitch_n = IS_ROWS ? 2 * TN + 32 : MAPS_PITCH;
+    constexpr int plane_m = (IS_ROWS ? KS : TM) * pitch_m, plane_n = (IS_ROWS ? KS : TN) * pitch_n;
+    __shared__ __attribute__((aligned(16))) char lds[NS * plane_m + plane_n];
+    char *const lds_x = lds + NS * plane_m;
+    const unsigned block = neighbour();
+    const long split = block / a.tiles, tile = block - split * a.tiles;
+    const long m0 = tile / a.tiles_n * TM, n0 = tile % a.tiles_n * TN;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wm = wave / 2 * (TM / 2), wn = wave % 2 * (TN / 2);
+    const bool bias = a.db && n0 == 0 && wn == 0;
+
+    // this thread's units: of dy, and of x from the other end of the workgroup
+    const int um = threadIdx.x, un = T - 1 - threadIdx.x;
+    const bool has_m = um < 2 * TM, has_n = un < 2 * TN;
+    Unit<B> dy;
+    Unit<1> x;
+    uint32_t scale = 0;
+    auto fetch = [&](long step) {
+        if constexpr (IS_ROWS) {
+            const long qm = step * KS + um / (TM / 32), qn = step * KS + un / (TN / 32);
+            const long om = m0 + 32 * (um % (TM / 32)), kn = n0 + 32 * (un % (TN / 32));
+            if (has_m) {
+                if (qm < a.n && om < a.c_out) dy.load(static_cast<const char *>(a.dy.p), (qm * a.dy.sn + om) * B, a.dy_end, (int)std::min<long>(32, a.c_out - om));
+                else dy.clear();
+            }
+            if (has_n) {
+                if (qn < a.n && kn < a.c) {
+                    x.load(reinterpret_cast<const char *>(a.x.codes), qn * a.x.sn + kn, a.codes_end, (int)std::min<long>(32, a.c - kn));
+                    scale = a.x.scales[qn * a.x.ssn + kn / 32];
                 } else {
-                    const float scale = Code8<CODE>::scale(a.x.scales[b * a.x.ssn + (rows ? k / 32 : k * a.x.ssc + m / 32)]);
-                    part = fmaf(dy, Code8<CODE>::value(a.x.codes[b * a.x.sn + (rows ? k : k * a.x.sc + m)], scale), part);
+                    x.clear();
+                    scale = 127;
                 }
             }
-            sum += part;
+        } else {
+            const long b = step / a.plane_steps, first = (step - b * a.plane_steps) * KS;
+            const long om = std::min(m0 + um / 2, a.c_out - 1), kn = std::min<long>(n0 + un / 2, a.c - 1);
+            const long pm = first + 32 * (um % 2), pn = first + 32 * (un % 2);
+            if (has_m) {
+                const int count = (int)std::min<long>(32, a.plane - pm);
+                if (count > 0) {
+                    dy.load(static_cast<const char *>(a.dy.p), (b * a.dy.sn + om * a.dy.sc + pm) * B, a.dy_end, count);
+                    if (count < 32) dy.keep(count);
+                } else {
+                    dy.clear();
+                }
+            }
+            if (has_n) {
+                const int count = (int)std::min<long>(32, a.plane - pn);
+                if (count > 0) {
+                    x.load(reinterpret_cast<const char *>(a.x.codes), b * a.x.sn + kn * a.x.sc + pn, a.codes_end, count);
+                    if (count < 32) x.keep(count);
+                    scale = a.x.scales[b * a.x.ssn + kn * a.x.ssc + pn / 32];
+                } else {
+                    x.clear();
+                    scale = 127;
+                }
+            }
         }
-        float *out = bias ? a.db + o : a.dw + i;
-        *out = a.accumulate ? *out + sum : sum;
+    };
+    auto put = [&] {
+        words4 w[4];
+        if (has_m) {
+            char *at = lds + (IS_ROWS ? um / (TM / 32) * pitch_m + 64 * (um % (TM / 32)) : um / 2 * pitch_m + 64 * (um % 2));
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                term<DT>(dy, n, w);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<words4 *>(at + n * plane_m + 16 * i) = w[i];
+            }
+        }
+        if (has_n) {
+            char *at = lds_x + (IS_ROWS ? un / (TN / 32) * pitch_n + 64 * (un % (TN / 32)) : un / 2 * pitch_n + 64 * (un % 2));
+            widen<CODE>(x, Code8<CODE>::scale(scale), w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<words4 *>(at + 16 * i) = w[i];
+        }
+    };
+
+    constexpr int IM = TM / 32, IN = TN / 32;           // 16 x 16 fragments of a wave
+    floatx4 acc[IM][IN], ones_acc[IM];
+#pragma unroll
+    for (int i = 0; i < IM; ++i) {
+        ones_acc[i] = floatx4{};
+#pragma unroll
+        for (int j = 0; j < IN; ++j) acc[i][j] = floatx4{};
     }
+    bf16x8 ones;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.f;
+    const long first = a.steps * split / a.splits, last = a.steps * (split + 1) / a.splits;
+    fetch(first);
+    for (long step = first; step < last; ++step) {
+        __syncthreads();                                // the step before has been read
+        put();
+        __syncthreads();
+        if (step + 1 < last) fetch(step + 1);
+#pragma unroll
+        for (int h = 0; h < KS; h += 32) {
+            bf16x8 v[IN];
+#pragma unroll
+            for (int j = 0; j < IN; ++j) v[j] = fragment<IS_ROWS>(lds_x, pitch_n, wn + 16 * j, h);
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < IM; ++i) {
+                    const bf16x8 u = fragment<IS_ROWS>(lds + n * plane_m, pitch_m, wm + 16 * i, h);
+#pragma unroll
+                    for (int j = 0; j < IN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, v[j], acc[i][j], 0, 0, 0);
+                    if (bias) ones_acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, ones, ones_acc[i], 0, 0, 0);
+                }
+        }
+    }
+    // lane l of a result holds column l % 16 of rows 4 (l / 16) ..
+    float *const dw = a.to + split * a.copy, *const db = a.splits > 1 ? dw + a.c_out * a.c : a.db;
+    const bool add = a.splits == 1 && a.accumulate;
+#pragma unroll
+    for (int i = 0; i < IM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const long o = m0 + wm + 16 * i + 4 * (lane >> 4) + r;
+            if (o >= a.c_out) continue;
+#pragma unroll
+            for (int j = 0; j < IN; ++j) {
+                const long k = n0 + wn + 16 * j + (lane & 15);
+                if (k < a.c) {
+                    float *at = dw + o * a.c + k;
+                    *at = add ? *at + acc[i][j][r] : acc[i][j][r];
+                }
+            }
+            if (bias && (lane & 15) == 0) db[o] = add ? db[o] + ones_acc[i][r] : ones_acc[i][r];
+        }
+}
+
+// dw and db (side by side in each copy) from the copies, or from none
+__global__ __launch_bounds__(256) void wgrad8_reduce_kernel(Wgrad8Launch a)
+{
+    __shared__ float sh[16][64];
+    const long weights = a.c_out * a.c, all = weights + (a.db ? a.c_out : 0);
+    for (long first = blockIdx.x * 64L; first < all; first += gridDim.x * 64L) {       // (every thread alike)
+        const long left = a.copy - first;
+        const float v = sum_copies64(a.scratch + first, a.copy, 0, (int)std::min<long>(left, 64), (int)a.splits, sh);
+        const long e = first + threadIdx.x;
+        if (threadIdx.x < 64 && e < all) {
+            float *at = e < weights ? a.dw + e : a.db + (e - weights);
+            *at = a.accumulate ? *at + v : v;
+        }
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(256) void wgrad8_clear_kernel(float *dw, float *db, long weights, long c_out)
+{
+    const long all = weights + (db ? c_out : 0);
+    for (long e = blockIdx.x * 256L + threadIdx.x; e < all; e += gridDim.x * 256L) (e < weights ? dw[e] : db[e - weights]) = 0.f;
+}
+
+template <int N> using num = std::integral_constant<int, N>;
+
+template <class F> void pick_tile(int tm, int tn, F f)
+{
+    if (tm == 128 && tn == 128) return f(num<128>{}, num<128>{});
+    if (tm == 128) return f(num<128>{}, num<64>{});
+    if (tn == 128) return f(num<64>{}, num<128>{});
+    return f(num<64>{}, num<64>{});
 }
 
 }  // namespace
 
-size_t wgrad8_scratch_floats(const NormSpan &, long) { return 0; }
-
-hipError_t launch_wgrad8(const Wgrad8Args &a, hipStream_t stream)
+size_t wgrad8_scratch_floats(const NormSpan &s, long c_out)
 {
-    const unsigned blocks = norm_blocks(a.c_out * (a.c + 1), 256);
-    pick_code(a.x.code, [&](auto code) {
-        if (a.dtype == 0) wgrad8_kernel<0, code()><<<blocks, 256, 0, stream>>>(a);
-        else if (a.dtype == 1) wgrad8_kernel<1, code()><<<blocks, 256, 0, stream>>>(a);
-        else wgrad8_kernel<2, code()><<<blocks, 256, 0, stream>>>(a);
-    });
-    return hipGetLastError();
+    if (s.n * s.plane == 0) return 0;
+    const Plan8 p = plan_of(s, c_out);
+    return p.splits > 1 ? (size_t)(p.splits * copy_floats(s, c_out)) : 0;
+}
+
+hipError_t launch_wgrad8(const Wgrad8Args &given, hipStream_t stream)
+{
+    Wgrad8Launch a;
+    static_cast<Wgrad8Args &>(a) = given;
+    const long weights = a.c_out * a.c;
+    if (a.n * a.plane == 0) {
+        if (!a.accumulate) wgrad8_clear_kernel<<<norm_blocks(weights + a.c_out, 256), 256, 0, stream>>>(a.dw, a.db, weights, a.c_out);
+        return hipGetLastError();
+    }
+    const Plan8 p = plan_of(a, a.c_out);
+    a.tiles_n = p.tiles_n; a.tiles = p.tiles_m * p.tiles_n; a.steps = p.steps; a.splits = p.splits;
+    a.plane_steps = (a.plane + KS - 1) / KS;
+    a.copy = copy_floats(a, a.c_out);
+    a.to = p.splits > 1 ? a.scratch : a.dw;
+    const bool rows = a.layout == ROWS;
+    const long size = a.dtype == 0 ? 4 : 2;
+    a.dy_end = size * ((a.n - 1) * a.dy.sn + (rows ? a.c_out : (a.c_out - 1) * a.dy.sc + a.plane));
+    a.codes_end = (a.n - 1) * a.x.sn + (rows ? a.c : (a.c - 1L) * a.x.sc + a.plane);
+    if (a.tiles * a.splits > 0x7fffffffL) return hipErrorInvalidValue;
+    const unsigned blocks = (unsigned)(a.tiles * a.splits);
+    auto type = [&](auto dt) {
+        pick_code(a.x.code, [&](auto code) {
+            pick_tile(p.tm, p.tn, [&](auto tm, auto tn) {
+                if (rows) wgrad8_kernel<dt(), code(), true, tm(), tn()><<<blocks, T, 0, stream>>>(a);
+                else wgrad8_kernel<dt(), code(), false, tm(), tn()><<<blocks, T, 0, stream>>>(a);
+            });
+        });
+    };
+    if (a.dtype == 0) type(num<0>{});
+    else if (a.dtype == 1) type(num<1>{});
+    else type(num<2>{});
+    Launches done;
+    if (done.failed() || p.splits == 1) return done.status();
+    wgrad8_reduce_kernel<<<norm_blocks(weights + a.c_out, 64), 256, 0, stream>>>(a);
+    return done.status();
 }
 
 }  // namespace sk
