@@ -1,51 +1,123 @@
 // Tensors into 8 bits and back.
-#include "act8_device.h"
+#include "act8_block.h"
 
 namespace sk {
 
 namespace {
 
-// A line and the block of it that a thread takes.
-struct Block8 {
-    long b, k, first;            // image or row, map, first element
-    int count;
-    __device__ __forceinline__ Block8(const NormSpan &s, long i)
+// HBM bounds both.  A lane takes eight values of a line, four lanes a block, and a wave U times as many, all of them asked for before the first is used.
+// LONG: a wave's values are of one line, whose place it works out on the scalar unit; a line takes as many waves as it needs.  Short lines: each lane works out
+// its own.
+template <bool LONG, int U> struct Octets {
+    struct At {
+        long b, k;               // image or row, map
+        long o;                  // octet of the line
+    };
+    const Pack8Args &a;
+    const Walk8 &w;
+    long line, o0;               // LONG: of the wave; else its first octet of all
+    __device__ __forceinline__ Octets(const Pack8Args &a_, const Walk8 &w_, long wave) : a(a_), w(w_)
     {
-        const long length = s.layout == ROWS ? s.c : s.plane, nb = blocks_of(length), line = i / nb;
-        first = 32 * (i - line * nb);
-        count = (int)(length - first < 32 ? length - first : 32);
-        b = s.layout == ROWS ? line : line / s.c;
-        k = s.layout == ROWS ? 0 : line - b * s.c;
+        if (LONG) {
+            line = wave / w.pieces;
+            o0 = (wave - line * w.pieces) * (64 * U);
+        } else {
+            line = 0;
+            o0 = wave * (64 * U);
+        }
     }
+    __device__ __forceinline__ At at(int u) const
+    {
+        const long o = o0 + 64 * u + (threadIdx.x & 63);
+        if (LONG) {
+            const long b = w.maps ? line / a.c : line;
+            return {b, line - b * a.c, o};
+        }
+        const long l = w.octets.divide(o), b = w.maps ? w.channels.divide(l) : l;
+        return {b, l - b * a.c, o - l * w.octets.by};
+    }
+    __device__ __forceinline__ bool there(const At &p) const { return LONG ? 8 * p.o < w.length : p.b < a.n; }
 };
-long all_blocks(const NormSpan &s) { return s.layout == ROWS ? s.n * blocks_of(s.c) : s.n * s.c * blocks_of(s.plane); }
 
-template <int DT, int CODE> __global__ __launch_bounds__(256) void pack8_kernel(Pack8Args a, long blocks)
+template <int DT, int CODE, bool LONG, int U> __global__ __launch_bounds__(256) void pack8_kernel(Pack8Args a, Walk8 w)
 {
-    typedef elem_t<DT> E;
-    constexpr uint32_t limit = Code8<CODE>::limit(DT);
-    for (long i = blockIdx.x * 256L + threadIdx.x; i < blocks; i += gridDim.x * 256L) {
-        const Block8 l(a, i);
-        const E *x = static_cast<const E *>(a.x.p) + l.b * a.x.sn + l.k * a.x.sc + l.first;
-        uint32_t most = 0;
-        for (int j = 0; j < l.count; ++j) most = max(most, counted((float)x[j], limit));
-        const uint32_t byte = Code8<CODE>::scale_byte(most);
-        a.packed.scales[l.b * a.packed.ssn + l.k * a.packed.ssc + l.first / 32] = (uint8_t)byte;
-        uint8_t *to = a.packed.codes + l.b * a.packed.sn + l.k * a.packed.sc + l.first;
-        for (int j = 0; j < l.count; ++j) to[j] = (uint8_t)any_code<CODE>((float)x[j], Code8<CODE>::inverse(byte), limit);
+    const long step = gridDim.x * 4L;
+    for (long wave = neighbour() * 4L + uniform(threadIdx.x >> 6); wave < w.waves; wave += step) {
+        const Octets<LONG, U> octets(a, w, wave);
+        Words<DT, 8> x[U];
+        int left[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const auto p = octets.at(u);
+            left[u] = octets.there(p) ? (int)std::min<long>(8, w.length - 8 * p.o) : 0;
+            load_octet<DT>(static_cast<src_t>(a.x.p) + sizeof(elem_t<DT>) * (p.b * a.x.sn + (w.maps ? p.k * a.x.sc : 0) + 8 * p.o), left[u], x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const auto p = octets.at(u);
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = x[u][j];
+            uint8_t *codes = a.packed.codes + p.b * a.packed.sn + (w.maps ? p.k * a.packed.sc : 0) + 8 * p.o;
+            uint8_t *scale = a.packed.scales + p.b * a.packed.ssn + (w.maps ? p.k * a.packed.ssc : 0) + p.o / 4;
+            put_octet<DT, CODE, 4>(f, left[u], codes, p.o % 4 == 0 ? scale : nullptr);
+        }
     }
 }
 
-template <int DT, int CODE> __global__ __launch_bounds__(256) void unpack8_kernel(Pack8Args a, long blocks)
+template <int DT, int CODE, bool LONG, int U> __global__ __launch_bounds__(256) void unpack8_kernel(Pack8Args a, Walk8 w)
 {
-    typedef elem_t<DT> E;
-    for (long i = blockIdx.x * 256L + threadIdx.x; i < blocks; i += gridDim.x * 256L) {
-        const Block8 l(a, i);
-        const float scale = Code8<CODE>::scale(a.packed.scales[l.b * a.packed.ssn + l.k * a.packed.ssc + l.first / 32]);
-        const uint8_t *from = a.packed.codes + l.b * a.packed.sn + l.k * a.packed.sc + l.first;
-        E *y = static_cast<E *>(a.x.p) + l.b * a.x.sn + l.k * a.x.sc + l.first;
-        for (int j = 0; j < l.count; ++j) y[j] = static_cast<E>(Code8<CODE>::value(from[j], scale));
+    const long step = gridDim.x * 4L;
+    for (long wave = neighbour() * 4L + uniform(threadIdx.x >> 6); wave < w.waves; wave += step) {
+        const Octets<LONG, U> octets(a, w, wave);
+        uint32_t c[U][2], scale[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const auto p = octets.at(u);
+            const int left = octets.there(p) ? (int)std::min<long>(8, w.length - 8 * p.o) : 0;
+            load_codes(a.packed.codes + p.b * a.packed.sn + (w.maps ? p.k * a.packed.sc : 0) + 8 * p.o, left, c[u]);
+            scale[u] = left > 0 ? a.packed.scales[p.b * a.packed.ssn + (w.maps ? p.k * a.packed.ssc : 0) + p.o / 4] : 127;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const auto p = octets.at(u);
+            const int left = octets.there(p) ? (int)std::min<long>(8, w.length - 8 * p.o) : 0;
+            float f[8];
+            octet_of_codes<CODE>(c[u], scale[u], f);
+            store_octet<DT>(static_cast<dst_t>(a.x.p) + sizeof(elem_t<DT>) * (p.b * a.x.sn + (w.maps ? p.k * a.x.sc : 0) + 8 * p.o), left, f);
+        }
     }
+}
+
+constexpr long kLongLine = 256;
+
+// f(LONG, U), and the walk
+template <class F> void pick_walk(const NormSpan &s, Walk8 &w, F f)
+{
+    w.maps = s.layout == MAPS;
+    w.length = w.maps ? s.plane : s.c;
+    const long lines = w.maps ? s.n * s.c : s.n, octets = 4 * blocks_of(w.length);
+    auto go = [&](auto is_long, auto u) {
+        if (is_long()) {
+            w.pieces = (octets + 64 * u() - 1) / (64 * u());
+            w.waves = lines * w.pieces;
+        } else {
+            w.octets = Divisor8(octets);
+            w.channels = Divisor8(s.c);
+            w.waves = (lines * octets + 64 * u() - 1) / (64 * u());
+        }
+        f(is_long, u);
+    };
+    typedef std::true_type Yes;
+    typedef std::false_type No;
+    typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, 2> Two;
+    typedef std::integral_constant<int, 4> Four;
+    if (w.length <= kLongLine) return lines * octets < 64 * 1024 ? go(No{}, One{}) : go(No{}, Two{});
+    // no piece is left half empty
+    if (octets <= 64) return go(Yes{}, One{});
+    if (octets <= 128 || lines * octets < 64 * 4096) return go(Yes{}, Two{});
+    return go(Yes{}, Four{});
 }
 
 template <class F> void pick_dtype(int dtype, F f)
@@ -59,15 +131,23 @@ template <class F> void pick_dtype(int dtype, F f)
 
 hipError_t launch_pack8(const Pack8Args &a, hipStream_t stream)
 {
-    const long blocks = all_blocks(a);
-    pick_dtype(a.dtype, [&](auto dt) { pick_code(a.packed.code, [&](auto code) { pack8_kernel<dt(), code()><<<norm_blocks(blocks, 256), 256, 0, stream>>>(a, blocks); }); });
+    Walk8 w;
+    pick_walk(a, w, [&](auto is_long, auto u) {
+        pick_dtype(a.dtype, [&](auto dt) {
+            pick_code(a.packed.code, [&](auto code) { pack8_kernel<dt(), code(), is_long(), u()><<<norm_blocks(w.waves, 4), 256, 0, stream>>>(a, w); });
+        });
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_unpack8(const Pack8Args &a, hipStream_t stream)
 {
-    const long blocks = all_blocks(a);
-    pick_dtype(a.dtype, [&](auto dt) { pick_code(a.packed.code, [&](auto code) { unpack8_kernel<dt(), code()><<<norm_blocks(blocks, 256), 256, 0, stream>>>(a, blocks); }); });
+    Walk8 w;
+    pick_walk(a, w, [&](auto is_long, auto u) {
+        pick_dtype(a.dtype, [&](auto dt) {
+            pick_code(a.packed.code, [&](auto code) { unpack8_kernel<dt(), code(), is_long(), u()><<<norm_blocks(w.waves, 4), 256, 0, stream>>>(a, w); });
+        });
+    });
     return hipGetLastError();
 }
 
