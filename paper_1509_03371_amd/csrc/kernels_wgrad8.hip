@@ -57,22 +57,40 @@ template <int B> struct Unit {                          // B bytes a value
 #pragma unroll
         for (int i = 0; i < 8 * B; ++i) w[i] = 0;
     }
-    // `count` values at `off` of an operand that spans `end` bytes.  Whole vectors where the operand goes on for as long; what they bring behind `count` is
-    // some other value of it.
+    __device__ __forceinline__ void vectors(const char *p)
+    {
+        typedef uint32_t Four __attribute__((ext_vector_type(4), aligned(1)));
+#pragma unroll
+        for (int i = 0; i < 2 * B; ++i) {
+            const Four v = reinterpret_cast<const Four *>(p)[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+        }
+    }
+    // the values from `by` bytes on, zeros behind them
+    __device__ __forceinline__ void down(int by)
+    {
+#pragma unroll
+        for (int step = 4 * B; step >= 1; step /= 2)
+#pragma unroll
+            for (int i = 0; i < 8 * B; ++i) w[i] = (by / 4) & step ? (i + step < 8 * B ? w[i + step < 8 * B ? i + step : 0] : 0) : w[i];
+        if (B < 4)
+#pragma unroll
+            for (int i = 0; i < 8 * B; ++i) w[i] = __builtin_amdgcn_alignbyte(i + 1 < 8 * B ? w[i + 1 < 8 * B ? i + 1 : 0] : 0, w[i], by & 3);
+    }
+    // `count` values at `off` of an operand that spans `end` bytes.  Whole vectors where the operand goes on for as long (what they bring behind `count` is
+    // some other value of it), else its last ones, moved down.
     __device__ __forceinline__ void load(const char *base, long off, long end, int count)
     {
         if (off + 32 * B <= end) {
-            typedef uint32_t Four __attribute__((ext_vector_type(4), aligned(1)));
-#pragma unroll
-            for (int i = 0; i < 2 * B; ++i) {
-                const Four v = reinterpret_cast<const Four *>(base + off)[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
-            }
-        } else {
+            vectors(base + off);
+        } else if (end >= 32 * B) {
+            vectors(base + end - 32 * B);
+            down((int)(off + 32 * B - end));
+        } else {                                        // an operand of fewer than 32 values
             clear();
 #pragma unroll 1
-            for (int j = 0; j < count; ++j) {           // (the operand's last values: a short loop, not many registers)
+            for (int j = 0; j < count; ++j) {
                 const char *p = base + off + B * j;
                 const uint32_t v = B == 1 ? *reinterpret_cast<const uint8_t *>(p) : B == 2 ? *reinterpret_cast<const uint16_t *>(p) : *reinterpret_cast<const uint32_t *>(p);
 #pragma unroll
