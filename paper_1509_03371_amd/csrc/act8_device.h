@@ -45,11 +45,15 @@ template <int CODE> struct Code8 {
             const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
             f[0] = lo[0] * scale; f[1] = lo[1] * scale; f[2] = hi[0] * scale; f[3] = hi[1] * scale;
         } else {
+// (unsigned bytes widen in one operation, whichever of the word's it is)
+            const uint32_t u = w ^ 0x80808080u;
+            f[0] = ((float)(u & 0xff) - 128.f) * scale;
+            f[1] = ((float)(u >> 8 & 0xff) - 128.f) * scale;
+            f[2] = ((float)(u >> 16 & 0xff) - 128.f) * scale;
+            f[3] = ((float)(u >> 24) - 128.f) * scale;
+            if ((u - 0x01010101u) & ~u & 0x80808080u)   // a byte of zero: NaN's code
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int q = (int)(w << (24 - 8 * i)) >> 24;
-                f[i] = q == -128 ? __builtin_nanf("") : (float)q * scale;
-            }
+                for (int i = 0; i < 4; ++i) f[i] = (u >> 8 * i & 0xff) ? f[i] : __builtin_nanf("");
         }
     }
     __device__ static __forceinline__ float value(uint32_t byte, float scale)

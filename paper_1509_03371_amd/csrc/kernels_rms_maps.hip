@@ -26,8 +26,10 @@ template <int DT, int P, int V, bool FAR> __device__ __forceinline__ void put_ma
     // s, then y: one piece of code for both
 #pragma unroll 1
     for (int last = 0; last < 2; ++last) {
-        const NormView &view = last ? a.y : a.sum;
-        const PackedView &packed = last ? a.y8 : a.sum8;
+        // (field by field: chosen as a whole, the arguments would be copied to memory first)
+        const NormView view = {last ? a.y.p : a.sum.p, last ? a.y.sn : a.sum.sn, last ? a.y.sc : a.sum.sc};
+        const PackedView packed = {last ? a.y8.codes : a.sum8.codes, last ? a.y8.scales : a.sum8.scales, last ? a.y8.sn : a.sum8.sn, last ? a.y8.sc : a.sum8.sc,
+                                   last ? a.y8.ssn : a.sum8.ssn, last ? a.y8.ssc : a.sum8.ssc, last ? a.y8.code : a.sum8.code};
         if (last) {
             if (!a.y.p && !a.y8.codes) return;
             float g[8];

@@ -29,16 +29,30 @@ template <int DT, int P, int V, bool FAR> struct NormedMaps<DT, P, V, FAR, true>
         const PackedView &v = a.s8;
         const int n = t.left > 0 ? t.channels(o) : 0;
         const uint8_t *scale = v.scales + t.b * v.ssn + t.first / 32 + (Off)(8 * o) * (Off)v.ssc + V * t.lane / 32;
+        const uint8_t *early = v.codes - V;            // (as Spot::load)
+        const Off off = t.offset(v.sc, 1, o) + (V - t.back);
         uint32_t byte[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             c[j] = 0;
             byte[j] = 127;
-            if (j < n) {
-                c[j] = load_line8<V>(v.codes + t.base(v.sn, v.sc, 1, j) + t.offset(v.sc, 1, o), t.left);
-                byte[j] = scale[j * v.ssc];
-            }
         }
+        if (n >= 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) c[j] = load_codes_of<V>(early + t.base(v.sn, v.sc, 1, j) + off);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) byte[j] = scale[j * v.ssc];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < n) {
+                    c[j] = load_codes_of<V>(early + t.base(v.sn, v.sc, 1, j) + off);
+                    byte[j] = scale[j * v.ssc];
+                }
+        }
+        if (t.back)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) c[j] >>= 8 * t.back;
 #pragma unroll
         for (int j = 0; j < 2; ++j) bytes[j] = byte[4 * j] | byte[4 * j + 1] << 8 | byte[4 * j + 2] << 16 | byte[4 * j + 3] << 24;
     }
@@ -61,7 +75,11 @@ template <int DT, int P, int V, bool FAR> struct NormedMaps<DT, P, V, FAR, true>
 template <int DT, int P, int V, bool FAR> __device__ __forceinline__ void rstd_of(const Spot<DT, P, V, FAR> &t, const RmsBwdArgs &a, float (&rstd)[V])
 {
     Words<0, V> w;
-    load_line<0, V>(reinterpret_cast<src_t>(a.rstd + t.position(0)), t.left, w);
+    w.clear();
+    if (t.left > 0) {
+        w.load(reinterpret_cast<src_t>(a.rstd + t.position(0) - t.back), 0);
+        if (t.back) move_down<0, V>(w, t.back);
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) rstd[i] = w[i];
 }
@@ -110,7 +128,7 @@ __device__ __forceinline__ void put_gradients(const Spot<DT, P, V, FAR> &t, cons
 }
 
 // Backwards; a workgroup keeps its threads' sums for dgamma in registers over its tiles, adds them up over its pixels' lanes at the end and writes a copy of them.
-template <int DT, int P, int V, int K, int T, bool HELD> __global__ __launch_bounds__(T) void rms_maps_bwd_kernel(RmsBwdArgs a, long tiles, long tiles_of_image)
+template <int DT, int P, int V, int K, int T, bool HELD> __global__ __launch_bounds__(T, DT == 0 ? 2 : 4) void rms_maps_bwd_kernel(RmsBwdArgs a, long tiles, long tiles_of_image)
 {
     __shared__ float part[T > 64 ? 2 * (T / 64) * P * V : 1];
     constexpr bool FAR = K == 0;

@@ -4,56 +4,32 @@
 
 namespace sk {
 
-// the first `left` of V elements side by side (V = 4: of a line of four or more), zeros behind them
-template <int DT, int V> __device__ __forceinline__ void load_line(src_t p, int left, Words<DT, V> &w)
+// V elements of a line that were read `back` elements early, because the line ends: moved down, zeros behind them
+template <int DT, int V> __device__ __forceinline__ void move_down(Words<DT, V> &w, int back)
 {
-    constexpr int S = sizeof(elem_t<DT>);
-    if (left >= V) {
-        w.load(p, 0);
-    } else if (left <= 0) {
-        w.clear();
-    } else {                                            // the line's last four, moved down
-        w.load(p - S * (V - left), 0);
-        if constexpr (V == 4 && DT == 0) {
-            if ((V - left) & 2) { w.w[0] = w.w[2]; w.w[1] = w.w[3]; w.w[2] = w.w[3] = 0; }
-            if ((V - left) & 1) { w.w[0] = w.w[1]; w.w[1] = w.w[2]; w.w[2] = w.w[3]; w.w[3] = 0; }
-        } else if constexpr (V == 4) {
-            const uint64_t v = ((uint64_t)w.w[1] << 32 | w.w[0]) >> 16 * (V - left);
-            w.w[0] = (uint32_t)v;
-            w.w[1] = (uint32_t)(v >> 32);
-        }
-    }
-}
-template <int DT, int V> __device__ __forceinline__ void store_line(dst_t p, int left, const float (&f)[V])
-{
-    constexpr int S = sizeof(elem_t<DT>);
-    if (left >= V) {
-        store_at<DT, V>(p, 0, f);
+    if constexpr (V == 4 && DT == 0) {
+        if (back & 2) { w.w[0] = w.w[2]; w.w[1] = w.w[3]; w.w[2] = w.w[3] = 0; }
+        if (back & 1) { w.w[0] = w.w[1]; w.w[1] = w.w[2]; w.w[2] = w.w[3]; w.w[3] = 0; }
     } else if constexpr (V == 4) {
-        if (left & 2) store_at<DT, 2>(p, 0, {f[0], f[1]});
-        if (left & 1) store_at<DT, 1>(p, S * (left & 2), {left & 2 ? f[2] : f[0]});
+        const uint64_t v = ((uint64_t)w.w[1] << 32 | w.w[0]) >> 16 * back;
+        w.w[0] = (uint32_t)v;
+        w.w[1] = (uint32_t)(v >> 32);
     }
 }
-template <int V> __device__ __forceinline__ uint32_t load_line8(const uint8_t *p, int left)
+// the first 1 to 3 of four elements
+template <int DT> __device__ __forceinline__ void store_some(dst_t p, int left, const float (&f)[4])
 {
-    typedef uint32_t Word __attribute__((ext_vector_type(1), aligned(1)));
-    if (left <= 0) return 0;
+    const float first = f[0], third = f[2];             // (values: a choice of places would put f into memory)
+    if (left & 2) store_at<DT, 2>(p, 0, {f[0], f[1]});
+    if (left & 1) store_at<DT, 1>(p, sizeof(elem_t<DT>) * (left & 2), {left & 2 ? third : first});
+}
+typedef uint32_t code_word __attribute__((ext_vector_type(1), aligned(1)));
+template <int V> __device__ __forceinline__ uint32_t load_codes_of(const uint8_t *p)
+{
     if (V == 1) return *p;
-    const uint32_t c = (*reinterpret_cast<const Word *>(p - (left < V ? V - left : 0)))[0];
-    return left < V ? c >> 8 * (V - left) : c;
+    return (*reinterpret_cast<const code_word *>(p))[0];
 }
-template <int V> __device__ __forceinline__ void store_line8(uint8_t *p, int left, uint32_t c)
-{
-    typedef uint32_t Word __attribute__((ext_vector_type(1), aligned(1)));
-    if (left >= V) {
-        if (V == 1) *p = (uint8_t)c;
-        else __builtin_nontemporal_store(Word{c}, reinterpret_cast<Word *>(p));
-    } else if (V == 4) {
-#pragma unroll
-        for (int j = 0; j < V - 1; ++j)
-            if (j < left) p[j] = (uint8_t)(c >> 8 * j);
-    }
-}
+
 // the largest of the lanes that hold a block's pixels: eight of four each, or four of one each
 template <int V> __device__ __forceinline__ uint32_t max_of_pixels(uint32_t v)
 {
@@ -72,7 +48,7 @@ template <int DT, int P, int V, bool FAR> struct Spot {
     const NormSpan &s;
     const int lane, octet0, octets;                     // octets: of the workgroup at a time
     long b, first;                                      // image, first pixel of the tile
-    int left;                                           // of this lane's pixels (0: none)
+    int left, back;                                     // of this lane's pixels (0: none); how much earlier it reads, so as not to read behind the line
     __device__ __forceinline__ explicit Spot(const NormSpan &s_) : s(s_), lane(threadIdx.x % P), octet0(threadIdx.x / P), octets(blockDim.x / P) {}
     __device__ __forceinline__ void go(long tile, long tiles_of_image)
     {
@@ -80,34 +56,51 @@ template <int DT, int P, int V, bool FAR> struct Spot {
         first = (tile - b * tiles_of_image) * (P * V);
         const long n = s.plane - first - V * lane;
         left = n >= V ? V : n > 0 ? (int)n : 0;
+        back = left > 0 ? V - left : 0;
     }
     // of an octet's channels: 8 and more = all, 0 and less = none
     __device__ __forceinline__ int channels(int o) const { return s.c - 8 * o; }
     // the lane's pixels in channel 8 o + j; `size` bytes an element
     __device__ __forceinline__ long base(long sn, long sc, int size, int j) const { return size * (b * sn + j * sc + first); }        // equal in all lanes
     __device__ __forceinline__ Off offset(long sc, int size, int o) const { return (Off)(8 * o) * (Off)(size * sc) + (Off)(size * V * lane); }
+    // zeros where there is nothing
     __device__ __forceinline__ void load(const NormView &v, int o, Words<DT, V> (&w)[8]) const
     {
         const int n = channels(o);
-        if (n >= 8) {
-            const Off off = offset(v.sc, S, o);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) load_line<DT, V>(static_cast<src_t>(v.p) + base(v.sn, v.sc, S, j) + off, left, w[j]);
+        for (int j = 0; j < 8; ++j) w[j].clear();
+        if (left <= 0 || n <= 0) return;
+        // V elements early and V - back on again: offsets of 32 bits are none below zero
+        const src_t early = static_cast<src_t>(v.p) - S * V;
+        const Off off = offset(v.sc, S, o) + S * (V - back);
+        if (n >= 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j].load(early + base(v.sn, v.sc, S, j) + off, 0);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                w[j].clear();
-                if (j < n) load_line<DT, V>(static_cast<src_t>(v.p) + base(v.sn, v.sc, S, j) + offset(v.sc, S, o), left, w[j]);
-            }
+            for (int j = 0; j < 8; ++j)
+                if (j < n) w[j].load(early + base(v.sn, v.sc, S, j) + off, 0);
         }
+        if (back)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) move_down<DT, V>(w[j], back);
     }
     __device__ __forceinline__ void store(const NormView &v, int o, const float (&f)[8][V]) const
     {
         const int n = channels(o);
         const Off off = offset(v.sc, S, o);
+        if (left >= V && n >= 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) store_at<DT, V>(static_cast<dst_t>(v.p) + base(v.sn, v.sc, S, j) + off, 0, f[j]);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j < n) store_line<DT, V>(static_cast<dst_t>(v.p) + base(v.sn, v.sc, S, j) + off, left, f[j]);
+            if (j < n) {
+                const dst_t p = static_cast<dst_t>(v.p) + base(v.sn, v.sc, S, j) + off;
+                if (left >= V) store_at<DT, V>(p, 0, f[j]);
+                else if constexpr (V == 4) store_some<DT>(p, left, f[j]);
+            }
     }
     // f in 8 bits.  All threads of the workgroup come here, with zeros where there is nothing; f does not outlive it.
     __device__ __forceinline__ void pack(const PackedView &v, int o, float (&f)[8][V]) const
@@ -158,11 +151,27 @@ template <int DT, int P, int V, bool FAR> struct Spot {
         }
         const Off at = offset(v.sc, 1, o);
         uint8_t *scale = v.scales + b * v.ssn + first / 32 + (Off)(8 * o) * (Off)v.ssc + V * lane / 32;
-        const bool leads = V * lane % 32 == 0 && left > 0;
+        const bool leads = V * lane % 32 == 0;
+        if (left >= V && n >= 8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint8_t *p = v.codes + base(v.sn, v.sc, 1, j) + at;
+                if (V == 1) *p = (uint8_t)c[j];
+                else __builtin_nontemporal_store(code_word{c[j]}, reinterpret_cast<code_word *>(p));
+            }
+            if (leads)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) scale[j * v.ssc] = (uint8_t)most[j];
+            return;
+        }
+        if (left <= 0) return;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n) {
-                store_line8<V>(v.codes + base(v.sn, v.sc, 1, j) + at, left, c[j]);
+                uint8_t *p = v.codes + base(v.sn, v.sc, 1, j) + at;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i < left) p[i] = (uint8_t)(c[j] >> 8 * i);
                 if (leads) scale[j * v.ssc] = (uint8_t)most[j];
             }
     }
