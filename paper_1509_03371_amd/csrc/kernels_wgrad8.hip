@@ -16,29 +16,38 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 // 8; fp32 24, three.  Each term is cut off, not rounded, so what is left is exact and no term overflows; an infinite value has no rest.
 template <int DT> constexpr int terms = DT == 1 ? 1 : DT == 2 ? 2 : 3;
 
-constexpr int KS = 64;                                  // positions of a step: two blocks of a map's line, or rows
-constexpr int MAPS_PITCH = 2 * KS + 16;                 // bytes from one channel to the next in LDS
-constexpr int T = 256;
+// A workgroup's tile: TM x TN output and input channels, KS positions at a time, WM x WN waves.  BIG ones take half as many bytes from the caches for each product and
+// keep two steps in LDS; small ones are for few weights or few positions.
+struct Tile8 {
+    int tm, tn;
+    bool big;
+};
+template <int DT, bool BIG> constexpr int step_of = BIG && terms<DT> > 1 ? 32 : 64;      // positions; two steps of fp32's terms fit the LDS at 32
+int step_positions(int dtype, bool big) { return big && dtype != 1 ? 32 : 64; }
 
 struct Plan8 {
-    int tm, tn;                                         // output and input channels of a workgroup's tile
-    long tiles_m, tiles_n, steps, splits;
+    Tile8 tile;
+    long tiles_m, tiles_n, plane_steps, steps, splits;
 };
 
-// As many workgroups as fill the card twice, so long as each takes four steps or more; tiles of 64 where those of 128 would be half empty or too few.
 Plan8 plan_of(const NormSpan &s, long c_out)
 {
     Plan8 p;
-    p.steps = s.layout == ROWS ? (s.n + KS - 1) / KS : s.n * ((s.plane + KS - 1) / KS);
-    const long most = std::max<long>(1, p.steps / 4);
-    auto count = [&](int tm, int tn) { return ((c_out + tm - 1) / tm) * ((s.c + tn - 1) / tn); };
-    p.tm = c_out <= 64 ? 64 : 128;
-    p.tn = s.c <= 64 ? 64 : 128;
-    if (count(p.tm, p.tn) * most < 256) p.tm = p.tn = 64;
-    p.tiles_m = (c_out + p.tm - 1) / p.tm;
-    p.tiles_n = (s.c + p.tn - 1) / p.tn;
-    const long tiles = p.tiles_m * p.tiles_n;
-    p.splits = std::min(most, std::max<long>(1, 512 / tiles));
+    auto lay = [&](int tm, int tn, bool big, long fill) {
+        const int ks = step_positions(s.dtype, big);
+        p.tile = {tm, tn, big};
+        p.plane_steps = (s.plane + ks - 1) / ks;
+        p.steps = s.layout == ROWS ? (s.n + ks - 1) / ks : s.n * p.plane_steps;
+        p.tiles_m = (c_out + tm - 1) / tm;
+        p.tiles_n = (s.c + tn - 1) / tn;
+        const long tiles = p.tiles_m * p.tiles_n, most = std::max<long>(1, p.steps / 4);       // four steps a workgroup or more
+        p.splits = std::min(most, std::max<long>(1, fill / tiles));
+        return tiles * p.splits;
+    };
+    // as many workgroups as fill the card: one a CU of big ones, else two
+    if (c_out >= 256 && s.c >= 256 && lay(256, 256, true, 256) >= 128 && p.splits <= 4) return p;
+    const int tm = c_out <= 64 ? 64 : 128, tn = s.c <= 64 ? 64 : 128;
+    if (lay(tm, tn, false, 512) < 256) lay(64, 64, false, 512);
     return p;
 }
 long copy_floats(const NormSpan &s, long c_out) { return (c_out * (s.c + 1) + 3) / 4 * 4; }
@@ -175,25 +184,27 @@ template <bool IS_ROWS> __device__ __forceinline__ bf16x8 fragment(const char *l
     }
 }
 
-// A workgroup takes TM x TN weights and a share of the positions, KS at a time: its threads load 32 values of a line each (of x a block with its scale), one step
-// ahead, widen them on their way into LDS, and four waves multiply, a quarter of the tile each.  db comes out of the same fragments, times ones.
-template <int DT, int CODE, bool IS_ROWS, int TM, int TN> __global__ __launch_bounds__(T) void wgrad8_kernel(Wgrad8Launch a)
+// A workgroup takes TM x TN weights and a share of the positions, KS at a time: its threads load 32 values of a line each (of x a block with its scale), a step
+// ahead, widen them on their way into LDS, and its waves multiply, a part of the tile each.  db comes out of the same fragments, times ones.
+template <int DT, int CODE, bool IS_ROWS, int TM, int TN, bool BIG> __global__ __launch_bounds__(BIG ? 512 : 256, 2) void wgrad8_kernel(Wgrad8Launch a)
 {
-    constexpr int NS = terms<DT>, B = DT == 0 ? 4 : 2;
-    constexpr int pitch_m = IS_ROWS ? 2 * TM + 32 : MAPS_PITCH, pitch_n = IS_ROWS ? 2 * TN + 32 : MAPS_PITCH;
-    constexpr int plane_m = (IS_ROWS ? KS : TM) * pitch_m, plane_n = (IS_ROWS ? KS : TN) * pitch_n;
-    __shared__ __attribute__((aligned(16))) char lds[NS * plane_m + plane_n];
-    char *const lds_x = lds + NS * plane_m;
+    constexpr int NS = terms<DT>, B = DT == 0 ? 4 : 2, T = BIG ? 512 : 256, KS = step_of<DT, BIG>;
+    constexpr int WN = 2, WM = T / 64 / WN, IM = TM / WM / 16, IN = TN / WN / 16;       // waves; 16 x 16 fragments of a wave
+    constexpr int per = KS / 32;                        // blocks of a map's line in a step
+    constexpr int pitch_m = IS_ROWS ? 2 * TM + 32 : 2 * KS + 16, pitch_n = IS_ROWS ? 2 * TN + 32 : 2 * KS + 16;
+    constexpr int plane_m = (IS_ROWS ? KS : TM) * pitch_m, plane_n = (IS_ROWS ? KS : TN) * pitch_n, buffer = NS * plane_m + plane_n;
+    extern __shared__ words4 smem8[];
+    char *const smem = reinterpret_cast<char *>(smem8);
     const unsigned block = neighbour();
     const long split = block / a.tiles, tile = block - split * a.tiles;
     const long m0 = tile / a.tiles_n * TM, n0 = tile % a.tiles_n * TN;
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int wm = wave / 2 * (TM / 2), wn = wave % 2 * (TN / 2);
+    const int wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
     const bool bias = a.db && n0 == 0 && wn == 0;
 
     // this thread's units: of dy, and of x from the other end of the workgroup
     const int um = threadIdx.x, un = T - 1 - threadIdx.x;
-    const bool has_m = um < 2 * TM, has_n = un < 2 * TN;
+    const bool has_m = um < TM * per, has_n = un < TN * per;
     Unit<B> dy;
     Unit<1> x;
     uint32_t scale = 0;
@@ -216,8 +227,8 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN> __global__ __launch_bo
             }
         } else {
             const long b = step / a.plane_steps, first = (step - b * a.plane_steps) * KS;
-            const long om = std::min(m0 + um / 2, a.c_out - 1), kn = std::min<long>(n0 + un / 2, a.c - 1);
-            const long pm = first + 32 * (um % 2), pn = first + 32 * (un % 2);
+            const long om = std::min(m0 + um / per, a.c_out - 1), kn = std::min<long>(n0 + un / per, a.c - 1);
+            const long pm = first + 32 * (um % per), pn = first + 32 * (un % per);
             if (has_m) {
                 const int count = (int)std::min<long>(32, a.plane - pm);
                 if (count > 0) {
@@ -240,10 +251,10 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN> __global__ __launch_bo
             }
         }
     };
-    auto put = [&] {
+    auto put = [&](char *lds) {
         words4 w[4];
         if (has_m) {
-            char *at = lds + (IS_ROWS ? um / (TM / 32) * pitch_m + 64 * (um % (TM / 32)) : um / 2 * pitch_m + 64 * (um % 2));
+            char *at = lds + (IS_ROWS ? um / (TM / 32) * pitch_m + 64 * (um % (TM / 32)) : um / per * pitch_m + 64 * (um % per));
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
                 term<DT>(dy, n, w);
@@ -252,14 +263,13 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN> __global__ __launch_bo
             }
         }
         if (has_n) {
-            char *at = lds_x + (IS_ROWS ? un / (TN / 32) * pitch_n + 64 * (un % (TN / 32)) : un / 2 * pitch_n + 64 * (un % 2));
+            char *at = lds + NS * plane_m + (IS_ROWS ? un / (TN / 32) * pitch_n + 64 * (un % (TN / 32)) : un / per * pitch_n + 64 * (un % per));
             widen<CODE>(x, Code8<CODE>::scale(scale), w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) *reinterpret_cast<words4 *>(at + 16 * i) = w[i];
         }
     };
 
-    constexpr int IM = TM / 32, IN = TN / 32;           // 16 x 16 fragments of a wave
     floatx4 acc[IM][IN], ones_acc[IM];
 #pragma unroll
     for (int i = 0; i < IM; ++i) {
@@ -270,18 +280,12 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN> __global__ __launch_bo
     bf16x8 ones;
 #pragma unroll
     for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.f;
-    const long first = a.steps * split / a.splits, last = a.steps * (split + 1) / a.splits;
-    fetch(first);
-    for (long step = first; step < last; ++step) {
-        __syncthreads();                                // the step before has been read
-        put();
-        __syncthreads();
-        if (step + 1 < last) fetch(step + 1);
+    auto multiply = [&](const char *lds) {
 #pragma unroll
         for (int h = 0; h < KS; h += 32) {
             bf16x8 v[IN];
 #pragma unroll
-            for (int j = 0; j < IN; ++j) v[j] = fragment<IS_ROWS>(lds_x, pitch_n, wn + 16 * j, h);
+            for (int j = 0; j < IN; ++j) v[j] = fragment<IS_ROWS>(lds + NS * plane_m, pitch_n, wn + 16 * j, h);
 #pragma unroll
             for (int n = 0; n < NS; ++n)
 #pragma unroll
@@ -291,6 +295,28 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN> __global__ __launch_bo
                     for (int j = 0; j < IN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, v[j], acc[i][j], 0, 0, 0);
                     if (bias) ones_acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, ones, ones_acc[i], 0, 0, 0);
                 }
+        }
+    };
+    const long first = a.steps * split / a.splits, last = a.steps * (split + 1) / a.splits;
+    fetch(first);
+    if constexpr (BIG) {
+        put(smem);
+        if (first + 1 < last) fetch(first + 1);
+        int now = 0;
+        for (long step = first; step < last; ++step) {
+            __syncthreads();                            // this step is in LDS, and the one before has been read
+            if (step + 1 < last) put(smem + (now ^ 1) * buffer);
+            if (step + 2 < last) fetch(step + 2);
+            multiply(smem + now * buffer);
+            now ^= 1;
+        }
+    } else {
+        for (long step = first; step < last; ++step) {
+            __syncthreads();                            // the step before has been read
+            put(smem);
+            __syncthreads();
+            if (step + 1 < last) fetch(step + 1);
+            multiply(smem);
         }
     }
     // lane l of a result holds column l % 16 of rows 4 (l / 16) ..
@@ -339,12 +365,22 @@ __global__ __launch_bounds__(256) void wgrad8_clear_kernel(float *dw, float *db,
 
 template <int N> using num = std::integral_constant<int, N>;
 
-template <class F> void pick_tile(int tm, int tn, F f)
+template <class F> void pick_tile(const Tile8 &t, F f)
 {
-    if (tm == 128 && tn == 128) return f(num<128>{}, num<128>{});
-    if (tm == 128) return f(num<128>{}, num<64>{});
-    if (tn == 128) return f(num<64>{}, num<128>{});
-    return f(num<64>{}, num<64>{});
+    typedef std::true_type Big;
+    typedef std::false_type Small;
+    if (t.big) return f(num<256>{}, num<256>{}, Big{});
+    if (t.tm == 128 && t.tn == 128) return f(num<128>{}, num<128>{}, Small{});
+    if (t.tm == 128) return f(num<128>{}, num<64>{}, Small{});
+    if (t.tn == 128) return f(num<64>{}, num<128>{}, Small{});
+    return f(num<64>{}, num<64>{}, Small{});
+}
+
+// bytes of LDS, as the kernel lays it out
+template <int DT, bool IS_ROWS, int TM, int TN, bool BIG> constexpr int lds_bytes()
+{
+    constexpr int KS = step_of<DT, BIG>;
+    return (BIG ? 2 : 1) * (IS_ROWS ? KS * (terms<DT> * (2 * TM + 32) + 2 * TN + 32) : (2 * KS + 16) * (terms<DT> * TM + TN));
 }
 
 }  // namespace
@@ -367,7 +403,7 @@ hipError_t launch_wgrad8(const Wgrad8Args &given, hipStream_t stream)
     }
     const Plan8 p = plan_of(a, a.c_out);
     a.tiles_n = p.tiles_n; a.tiles = p.tiles_m * p.tiles_n; a.steps = p.steps; a.splits = p.splits;
-    a.plane_steps = (a.plane + KS - 1) / KS;
+    a.plane_steps = p.plane_steps;
     a.copy = copy_floats(a, a.c_out);
     a.to = p.splits > 1 ? a.scratch : a.dw;
     const bool rows = a.layout == ROWS;
@@ -376,18 +412,24 @@ hipError_t launch_wgrad8(const Wgrad8Args &given, hipStream_t stream)
     a.codes_end = (a.n - 1) * a.x.sn + (rows ? a.c : (a.c - 1L) * a.x.sc + a.plane);
     if (a.tiles * a.splits > 0x7fffffffL) return hipErrorInvalidValue;
     const unsigned blocks = (unsigned)(a.tiles * a.splits);
+    Launches done;
     auto type = [&](auto dt) {
         pick_code(a.x.code, [&](auto code) {
-            pick_tile(p.tm, p.tn, [&](auto tm, auto tn) {
-                if (rows) wgrad8_kernel<dt(), code(), true, tm(), tn()><<<blocks, T, 0, stream>>>(a);
-                else wgrad8_kernel<dt(), code(), false, tm(), tn()><<<blocks, T, 0, stream>>>(a);
+            pick_tile(p.tile, [&](auto tm, auto tn, auto big) {
+                auto go = [&](auto is_rows) {
+                    constexpr int lds = lds_bytes<dt(), is_rows(), tm(), tn(), big()>();
+                    auto *kernel = wgrad8_kernel<dt(), code(), is_rows(), tm(), tn(), big()>;
+                    if (lds > 65536 && done.failed(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds))) return;
+                    kernel<<<blocks, big() ? 512 : 256, lds, stream>>>(a);
+                };
+                if (rows) go(std::true_type{});
+                else go(std::false_type{});
             });
         });
     };
     if (a.dtype == 0) type(num<0>{});
     else if (a.dtype == 1) type(num<1>{});
     else type(num<2>{});
-    Launches done;
     if (done.failed() || p.splits == 1) return done.status();
     wgrad8_reduce_kernel<<<norm_blocks(weights + a.c_out, 64), 256, 0, stream>>>(a);
     return done.status();

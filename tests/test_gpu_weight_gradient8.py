@@ -88,3 +88,19 @@ def test_no_positions():
         assert (dw == 2).all() and (db == 2).all()
         B.weight_gradient8(dy, p, dw=dw, db=db)
         assert (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("positions,c,c_out", [((701,), 2050, 2101), ((3, 230), 2050, 2101), ((150,), 3000, 2900)], ids=str)
+def test_many_weights(positions, c, c_out, kind, code):
+    """Enough weights for the largest tiles, which end inside the tensors."""
+    from paper_1509_03371_amd import binding as B
+    x, dy = case(positions, c, c_out, kind, 97, 3 if kind == "f16" else 0)
+    p = B.pack8(x, code, axis=1)
+    dw, db = B.weight_gradient8(dy, p)
+    rw, rb, ew, eb = product_bounds(to64(dy), to64(B.unpack8(p)))
+    close(dw, rw, ew, "dw")
+    close(db, rb, eb, "db")
+    again = B.weight_gradient8(dy, p)
+    assert torch.equal(again[0], dw) and torch.equal(again[1], db), "two equal calls"
