@@ -476,12 +476,12 @@ sk_status sknet_layer_norm_backward(const sk_extent *extent, const sk_view *dy, 
  *   SK_I8  : Q = 127; two's complement of -127 .. 127, -128 = NaN.
  * So a value is off by at most half a step: SK_E4M3 2^-4 of itself or 2^(k-10) (values below 2^(k-6)), SK_I8 2^(k-1) < largest / 126.  Infinite and NaN elements
  * become NaN and leave the others of their block as they are: the largest is taken over the finite ones.  Magnitudes beyond the largest that
- * a code can stand for in the extent's dtype are limited to it (SK_F16: 61440 and 65024, else 1.875 * 2^127 and 127 * 2^121), so that finite values stay finite.
+ * a code can stand for in the extent's dtype are limited to it (SK_F16: 61440 and 65024, else 1.875 * 2^127 and 127 * 2^120), so that finite values stay finite.
  * What a code stands for is exact in bf16.
  *
  * codes: element (position, channel) is the byte at the place that an sk_view of these strides gives it.  scales: of the line of row b, or of map k
  * of image b, at b*scale_stride_n (+ k*scale_stride_c), one byte for each block, side by side.  Lines of a result must not overlap (SK_ESHAPE).  scales
- * that sknet_unpack8 or another call reads may hold any byte 10 .. 248; other scales, which no call here writes, give unspecified values.
+ * that sknet_unpack8 or another call reads may hold any byte 10 .. 247; other scales, which no call here writes, give unspecified values.
  *
  * Extents, views, in-place results, streams and graphs as above; results (codes and scales, fp32 values and the workspace among them) must not
  * overlap anything else of the call (SK_EINVAL) but where a view may be another's place.  Operands of equal strides in bytes are compared line by

@@ -5,7 +5,7 @@ import numpy as np
 TOP = {"e4m3": 448.0, "i8": 127.0}
 NAN = {"e4m3": 0x7F, "i8": 0x80}
 # the largest magnitude that a code can stand for: in fp16, and in fp32 and bf16
-LIMIT = {("e4m3", "f16"): 61440.0, ("i8", "f16"): 65024.0, ("e4m3", "f32"): 1.875 * 2.0 ** 127, ("i8", "f32"): 127 * 2.0 ** 121}
+LIMIT = {("e4m3", "f16"): 61440.0, ("i8", "f16"): 65024.0, ("e4m3", "f32"): 1.875 * 2.0 ** 127, ("i8", "f32"): 127 * 2.0 ** 120}
 
 
 def e4m3_table():

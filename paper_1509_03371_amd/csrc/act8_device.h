@@ -10,10 +10,10 @@ template <int CODE> struct Code8 {
     static constexpr uint32_t top = CODE == E4M3 ? 0x600000 : 0x7e0000;     // mantissa of Q: 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6
     static constexpr int down = CODE == E4M3 ? 8 : 6;                       // exponent of Q
     static constexpr uint32_t nan = CODE == E4M3 ? 0x7f : 0x80;
-    // the largest magnitude that a code can stand for in a type: 61440, 65024; 1.875 * 2^127, 127 * 2^121
+    // the largest magnitude that a code can stand for in a type: 61440, 65024; 1.875 * 2^127, 127 * 2^120
     __host__ __device__ static constexpr uint32_t limit(int dt)
     {
-        return dt == 2 ? (CODE == E4M3 ? 0x47700000u : 0x477e0000u) : (CODE == E4M3 ? 0x7f700000u : 0x7f7e0000u);
+        return dt == 2 ? (CODE == E4M3 ? 0x47700000u : 0x477e0000u) : (CODE == E4M3 ? 0x7f700000u : 0x7efe0000u);
     }
     // k + 127 for a block whose largest magnitude has these bits: one more than its exponent if its mantissa is over Q's
     __device__ static __forceinline__ uint32_t scale_byte(uint32_t largest)
@@ -37,24 +37,38 @@ template <int CODE> struct Code8 {
         }
     }
     __device__ static __forceinline__ uint32_t one(float v, float inverse) { return four(v, 0.f, 0.f, 0.f, inverse) & 0xff; }
-    // four values
-    __device__ static __forceinline__ void values(uint32_t w, float scale, float (&f)[4])
+    // four values, NaN left out of account
+    __device__ static __forceinline__ void numbers(uint32_t w, float scale, float (&f)[4])
     {
         if constexpr (CODE == E4M3) {
             typedef float floatx2 __attribute__((ext_vector_type(2)));
             const floatx2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
             f[0] = lo[0] * scale; f[1] = lo[1] * scale; f[2] = hi[0] * scale; f[3] = hi[1] * scale;
-        } else {
-// (unsigned bytes widen in one operation, whichever of the word's it is)
+        } else {                 // unsigned bytes widen in one operation, whichever of the word's it is; 128 too much, which the sum takes off again, exactly
             const uint32_t u = w ^ 0x80808080u;
-            f[0] = ((float)(u & 0xff) - 128.f) * scale;
-            f[1] = ((float)(u >> 8 & 0xff) - 128.f) * scale;
-            f[2] = ((float)(u >> 16 & 0xff) - 128.f) * scale;
-            f[3] = ((float)(u >> 24) - 128.f) * scale;
-            if ((u - 0x01010101u) & ~u & 0x80808080u)   // a byte of zero: NaN's code
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f[i] = (u >> 8 * i & 0xff) ? f[i] : __builtin_nanf("");
+            const float below = -128.f * scale;
+            f[0] = fmaf((float)(u & 0xff), scale, below);
+            f[1] = fmaf((float)(u >> 8 & 0xff), scale, below);
+            f[2] = fmaf((float)(u >> 16 & 0xff), scale, below);
+            f[3] = fmaf((float)(u >> 24), scale, below);
         }
+    }
+    // is one of the four NaN, and `numbers` wrong about it?  (a byte of zero, of -128 + 128)
+    __device__ static __forceinline__ uint32_t unlike(uint32_t w)
+    {
+        const uint32_t u = w ^ 0x80808080u;
+        return CODE == E4M3 ? 0 : (u - 0x01010101u) & ~u & 0x80808080u;
+    }
+    __device__ static __forceinline__ void mark(uint32_t w, float (&f)[4])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = (w >> 8 * i & 0xff) == nan ? __builtin_nanf("") : f[i];
+    }
+    // four values
+    __device__ static __forceinline__ void values(uint32_t w, float scale, float (&f)[4])
+    {
+        numbers(w, scale, f);
+        if (unlike(w)) mark(w, f);
     }
     __device__ static __forceinline__ float value(uint32_t byte, float scale)
     {

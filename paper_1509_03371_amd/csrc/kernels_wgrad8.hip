@@ -45,7 +45,7 @@ Plan8 plan_of(const NormSpan &s, long c_out)
         return tiles * p.splits;
     };
     // as many workgroups as fill the card: one a CU of big ones, else two
-    if (c_out >= 256 && s.c >= 256 && lay(256, 256, true, 256) >= 128 && p.splits <= 4) return p;
+    if (s.dtype != 1 && c_out >= 256 && s.c >= 256 && lay(256, 256, true, 256) >= 128 && p.splits <= 4) return p;
     const int tm = c_out <= 64 ? 64 : 128, tn = s.c <= 64 ? 64 : 128;
     if (lay(tm, tn, false, 512) < 256) lay(64, 64, false, 512);
     return p;
@@ -120,6 +120,7 @@ template <int B> struct Unit {                          // B bytes a value
 
 template <int CODE> __device__ __forceinline__ void widen(const Unit<1> &u, float scale, words4 (&to)[4])
 {
+    uint32_t odd = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if constexpr (CODE == E4M3) {
@@ -127,12 +128,17 @@ template <int CODE> __device__ __forceinline__ void widen(const Unit<1> &u, floa
             to[i / 2][2 * (i % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u.w[i], scale, true));
         } else {
             float f[4];
-            Code8<CODE>::values(u.w[i], scale, f);
+            Code8<CODE>::numbers(u.w[i], scale, f);
+            odd |= Code8<CODE>::unlike(u.w[i]);
             // exact: the upper halves are the values
             to[i / 2][2 * (i % 2)] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302);
             to[i / 2][2 * (i % 2) + 1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302);
         }
     }
+    if (odd)
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if ((u.w[i / 4] >> 8 * (i % 4) & 0xff) == Code8<CODE>::nan) to[i / 8][i / 2 % 4] |= 0x7fc0u << 16 * (i % 2);
 }
 
 __device__ __forceinline__ float rest(float v) { return magnitude(v) == 0x7f800000u ? 0.f : v - __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
@@ -307,7 +313,9 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN, bool BIG> __global__ _
             __syncthreads();                            // this step is in LDS, and the one before has been read
             if (step + 1 < last) put(smem + (now ^ 1) * buffer);
             if (step + 2 < last) fetch(step + 2);
+            __builtin_amdgcn_s_setprio(1);
             multiply(smem + now * buffer);
+            __builtin_amdgcn_s_setprio(0);
             now ^= 1;
         }
     } else {
@@ -316,7 +324,9 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN, bool BIG> __global__ _
             put(smem);
             __syncthreads();
             if (step + 1 < last) fetch(step + 1);
+            __builtin_amdgcn_s_setprio(1);
             multiply(smem);
+            __builtin_amdgcn_s_setprio(0);
         }
     }
     // lane l of a result holds column l % 16 of rows 4 (l / 16) ..
