@@ -293,6 +293,16 @@ def _orders(shape, strides, axis):
 
 
 @functools.lru_cache(maxsize=4096)
+def _common_order(shape, strides, axis, order):
+    """The first order that tensors of these sizes, with strides each, have in common (order: that one alone), and their strides in it; None if there is none."""
+    choices = [_orders(shape, s, axis) for s in strides]
+    for o in choices[0]:
+        if (order is None or o == order) and all(o in c for c in choices):
+            return o, [c[o] for c in choices]
+    return None
+
+
+@functools.lru_cache(maxsize=4096)
 def _workspace(dtype, layout, n, c, plane):
     """Bytes of a backward call's workspace: a matter of the extent alone."""
     need = C.c_uint64()
@@ -340,33 +350,31 @@ class _Operator:
 
     def place(self, order=None, **tensors):
         """Find the order that the tensors have in common (order: that one alone); returns the extent, and their views by name (None for None)."""
-        x, axis = self.x, self.axis
-        choices = _orders(x.shape, x.stride(), axis)
-        if order is not None:
-            choices = {o: strides for o, strides in choices.items() if o == order}
-        theirs = {}
+        x = self.x
+        shape, dtype, device = x.shape, x.dtype, self.device
+        strides, places = [x.stride()], []
         for name, t in tensors.items():
-            if t is None or t is x:
-                continue
-            if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == x.dtype):
-                raise TypeError("%s must be a tensor of %s on %s" % (name, x.dtype, self.device))
-            if t.shape != x.shape:
-                raise ValueError("%s has shape %s instead of %s" % (name, tuple(t.shape), tuple(x.shape)))
-            theirs[name] = _orders(t.shape, t.stride(), axis)
-        for order in choices:
-            if all(order in o for o in theirs.values()):
-                break
-        else:
+            if t is None:
+                places.append(None)
+            elif t is x:
+                places.append(0)
+            else:
+                if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype):
+                    raise TypeError("%s must be a tensor of %s on %s" % (name, dtype, device))
+                if t.shape != shape:
+                    raise ValueError("%s has shape %s instead of %s" % (name, tuple(t.shape), tuple(shape)))
+                places.append(len(strides))
+                strides.append(t.stride())
+        found = _common_order(shape, tuple(strides), self.axis, order)
+        if found is None:
+            theirs = sorted(n for n, p in zip(tensors, places) if p)
             raise ValueError("%s, strides %s, keep the channels of axis %d neither as rows nor as maps in common; make them contiguous" % (
-                ", ".join([self.what] + sorted(theirs)), [x.stride()] + [tensors[n].stride() for n in sorted(theirs)], axis))
-        layout, n, c, plane = order
-        self.order = order
-        self.extent = SkExtent(_OP_TYPES[x.dtype], layout, n, c, plane)
-        out = [SkView(x.data_ptr(), *choices[order])]
-        for name, t in tensors.items():
-            out.append(None if t is None else out[0] if t is x else SkView(t.data_ptr(), *theirs[name][order]))
-        self.held = out
-        return [None if v is None else C.byref(v) for v in out]
+                ", ".join([self.what] + theirs), [x.stride()] + [tensors[n].stride() for n in theirs], self.axis))
+        self.order, steps = found
+        self.extent = SkExtent(_OP_TYPES[dtype], *self.order)
+        first = SkView(x.data_ptr(), *steps[0])
+        self.held = [None if p is None else first if p == 0 else SkView(t.data_ptr(), *steps[p]) for p, t in zip(places, tensors.values())]
+        return [C.byref(first)] + [None if v is None else C.byref(v) for v in self.held]
 
     def values(self, t, count, name):
         """DEVICE pointer of `count` fp32 values, None for None."""

@@ -1,7 +1,6 @@
 // Host side of activations in 8 bits, root-mean-square norm and the weight gradient over inputs in 8 bits.  See include/sknet.h for the contract.
 #include <cmath>
 #include <utility>
-#include <vector>
 
 #include "act8.h"
 #include "operand_checks.h"
@@ -62,8 +61,8 @@ public:
         sk_extent e = e_;
         if (c) e.c = c;
         SK_TRY(check_view(who_, name, e, v, result));
-        all_.push_back(lines(name, v->data, e, e.c, v->stride_n, v->stride_c, element_bytes(e), false, result));
-        all_.back().view = v;
+        add(lines(name, v->data, e, e.c, v->stride_n, v->stride_c, element_bytes(e), false, result));
+        all_[count_ - 1].view = v;
         return SK_OK;
     }
     sk_status packed(const char *name, const sk_packed *p, bool result)
@@ -77,7 +76,7 @@ public:
             const Operand l = lines(name, o.p, e_, e_.c, o.sn, o.sc, 1, o.blocks, result);
             if (l.end() - l.at() > kMaxElements) return fail(SK_EUNSUPPORTED, "%s: %s reaches over more than 2^46 bytes", who_, name);
             if (result && !l.apart(l.line)) return fail(SK_ESHAPE, "%s: lines of %s overlap", who_, name);
-            all_.push_back(l);
+            add(l);
         }
         return SK_OK;
     }
@@ -85,21 +84,21 @@ public:
     {
         if (!p) return SK_OK;
         if (reinterpret_cast<uintptr_t>(p) % 4) return fail(SK_EINVAL, "%s: %s is not aligned to its elements", who_, name);
-        all_.push_back(flat(name, p, 4 * count, result));
+        add(flat(name, p, 4 * count, result));
         return SK_OK;
     }
     sk_status workspace(const void *p, uint64_t bytes, uint64_t need)
     {
         if (need && (!p || bytes < need)) return fail(SK_EINVAL, "%s: needs a workspace of %llu bytes", who_, (unsigned long long)need);
         if (reinterpret_cast<uintptr_t>(p) % 16) return fail(SK_EINVAL, "%s: the workspace is not aligned to 16 bytes", who_);
-        if (need) all_.push_back(flat("the workspace", p, need, true));
+        if (need) add(flat("the workspace", p, need, true));
         return SK_OK;
     }
     // places: views that an input may give to a result, element for element
     sk_status settle(std::initializer_list<const sk_view *> places = {}) const
     {
-        for (size_t i = 0; i < all_.size(); ++i)
-            for (size_t j = 0; j < all_.size(); ++j) {
+        for (int i = 0; i < count_; ++i)
+            for (int j = 0; j < count_; ++j) {
                 const Operand &a = all_[i], &b = all_[j];
                 if (i == j || !a.result || (b.result && j < i) || disjoint(a, b)) continue;
                 bool place = false;
@@ -113,7 +112,10 @@ public:
 private:
     const char *who_;
     const sk_extent &e_;
-    std::vector<Operand> all_;
+    static constexpr int kMost = 16;                    // a call has no more operands than this, codes and scales apart
+    Operand all_[kMost];
+    int count_ = 0;
+    void add(const Operand &o) { all_[count_++] = o; }
 };
 
 sk::PackedView take_packed(const sk_packed *p)
@@ -134,16 +136,6 @@ sk_status check_c_out(const char *who, const sk_extent &e, int64_t c_out)
     if (c_out > kMaxChannels || (__int128)e.c * c_out > kMaxPositions) return fail(SK_EUNSUPPORTED, "%s: more than 2^27 output channels or 2^40 weights", who);
     if ((__int128)e.n * e.plane * c_out > kMaxElements) return fail(SK_EUNSUPPORTED, "%s: more than 2^46 elements", who);
     return SK_OK;
-}
-
-// host memory for the list of operands is the one thing that can run out here
-template <class F> sk_status guarded(const char *who, F f)
-{
-    try {
-        return f();
-    } catch (const std::exception &) {
-        return fail(SK_ENOMEM, "%s: out of host memory", who);
-    }
 }
 
 sk_status change8(const char *who, const sk_extent *extent, const sk_view *x, const sk_packed *packed, bool pack, void *hip_stream)
@@ -172,48 +164,46 @@ extern "C" {
 
 sk_status sknet_pack8(const sk_extent *extent, const sk_view *x, const sk_packed *packed, void *hip_stream)
 {
-    return guarded("pack8", [&] { return change8("pack8", extent, x, packed, true, hip_stream); });
+    return change8("pack8", extent, x, packed, true, hip_stream);
 }
 
 sk_status sknet_unpack8(const sk_extent *extent, const sk_packed *packed, const sk_view *y, void *hip_stream)
 {
-    return guarded("unpack8", [&] { return change8("unpack8", extent, y, packed, false, hip_stream); });
+    return change8("unpack8", extent, y, packed, false, hip_stream);
 }
 
 sk_status sknet_rms_norm(const sk_extent *extent, const sk_view *x, const sk_view *residual, const float *gamma_dev, float eps, const sk_view *sum,
                          const sk_packed *sum8, const sk_view *y, const sk_packed *y8, float *rstd_dev, void *hip_stream)
 {
     const char *who = "rms_norm";
-    return guarded(who, [&]() -> sk_status {
-        bool empty = false;
-        SK_TRY(check_extent(who, extent, &empty));
-        if (!x) return fail(SK_EINVAL, "%s: null argument", who);
-        if (!sum && !sum8 && !y && !y8 && !rstd_dev) return fail(SK_EINVAL, "%s: no result is asked for", who);
-        if (!(eps > 0.f) || !std::isfinite(eps)) return fail(SK_EINVAL, "%s: eps must be positive and finite", who);
-        if (empty) return SK_OK;
-        const sk_extent &e = *extent;
-        Operands all(who, e);
-        SK_TRY(all.view("x", x, false));
-        SK_TRY(all.view("residual", residual, false));
-        SK_TRY(all.view("sum", sum, true));
-        SK_TRY(all.packed("sum8", sum8, true));
-        SK_TRY(all.view("y", y, true));
-        SK_TRY(all.packed("y8", y8, true));
-        SK_TRY(all.values("gamma", gamma_dev, e.c, false));
-        SK_TRY(all.values("rstd", rstd_dev, (__int128)e.n * e.plane, true));
-        SK_TRY(all.settle({x, residual}));
-        sk::RmsArgs a{};
-        take_span(e, &a);
-        a.x = take_view(x);
-        a.residual = take_view(residual);
-        a.sum = take_view(sum);
-        a.sum8 = take_packed(sum8);
-        a.y = take_view(y);
-        a.y8 = take_packed(y8);
-        a.gamma = gamma_dev; a.rstd = rstd_dev; a.eps = eps;
-        SK_HIP(sk::launch_rms_norm(a, static_cast<hipStream_t>(hip_stream)));
-        return SK_OK;
-    });
+    bool empty = false;
+    SK_TRY(check_extent(who, extent, &empty));
+    if (!x) return fail(SK_EINVAL, "%s: null argument", who);
+    if (!sum && !sum8 && !y && !y8 && !rstd_dev) return fail(SK_EINVAL, "%s: no result is asked for", who);
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(SK_EINVAL, "%s: eps must be positive and finite", who);
+    if (empty) return SK_OK;
+    const sk_extent &e = *extent;
+    Operands all(who, e);
+    SK_TRY(all.view("x", x, false));
+    SK_TRY(all.view("residual", residual, false));
+    SK_TRY(all.view("sum", sum, true));
+    SK_TRY(all.packed("sum8", sum8, true));
+    SK_TRY(all.view("y", y, true));
+    SK_TRY(all.packed("y8", y8, true));
+    SK_TRY(all.values("gamma", gamma_dev, e.c, false));
+    SK_TRY(all.values("rstd", rstd_dev, (__int128)e.n * e.plane, true));
+    SK_TRY(all.settle({x, residual}));
+    sk::RmsArgs a{};
+    take_span(e, &a);
+    a.x = take_view(x);
+    a.residual = take_view(residual);
+    a.sum = take_view(sum);
+    a.sum8 = take_packed(sum8);
+    a.y = take_view(y);
+    a.y8 = take_packed(y8);
+    a.gamma = gamma_dev; a.rstd = rstd_dev; a.eps = eps;
+    SK_HIP(sk::launch_rms_norm(a, static_cast<hipStream_t>(hip_stream)));
+    return SK_OK;
 }
 
 sk_status sknet_rms_norm_workspace(const sk_extent *extent, uint64_t *bytes)
@@ -232,41 +222,39 @@ sk_status sknet_rms_norm_backward(const sk_extent *extent, const sk_view *dy, co
                                   uint64_t workspace_bytes, void *hip_stream)
 {
     const char *who = "rms_norm_backward";
-    return guarded(who, [&]() -> sk_status {
-        bool empty = false;
-        SK_TRY(check_extent(who, extent, &empty));
-        if (!dy || !s == !s8) return fail(SK_EINVAL, "%s: needs dy, and either s or s8", who);
-        const sk_extent &e = *extent;
-        sk::RmsBwdArgs a{};
-        take_span(e, &a);
-        Operands all(who, e);
-        SK_TRY(all.values("dgamma", dgamma_dev, e.c, true));
-        SK_TRY(all.values("gamma", gamma_dev, e.c, false));
-        if (!empty) {
-            if (!rstd_dev) return fail(SK_EINVAL, "%s: needs the forward pass's rstd", who);
-            SK_TRY(all.view("dy", dy, false));
-            SK_TRY(all.view("s", s, false));
-            SK_TRY(all.packed("s8", s8, false));
-            SK_TRY(all.view("dsum", dsum, false));
-            SK_TRY(all.view("dx", dx, true));
-            SK_TRY(all.values("rstd", rstd_dev, (__int128)e.n * e.plane, false));
-            const uint64_t need = dgamma_dev ? sizeof(float) * (uint64_t)sk::rms_bwd_scratch_floats(a) : 0;
-            SK_TRY(all.workspace(workspace_dev, workspace_bytes, need));
-            a.dy = take_view(dy);
-            a.s = take_view(s);
-            a.s8 = take_packed(s8);
-            a.dsum = take_view(dsum);
-            a.dx = take_view(dx);
-            a.rstd = rstd_dev;
-            a.scratch = static_cast<float *>(workspace_dev);
-            a.scratch_floats = (size_t)(need / sizeof(float));
-        }
-        SK_TRY(all.settle({dy, s, dsum}));
-        a.gamma = gamma_dev;
-        a.dgamma = dgamma_dev;
-        SK_HIP(sk::launch_rms_norm_bwd(a, static_cast<hipStream_t>(hip_stream)));
-        return SK_OK;
-    });
+    bool empty = false;
+    SK_TRY(check_extent(who, extent, &empty));
+    if (!dy || !s == !s8) return fail(SK_EINVAL, "%s: needs dy, and either s or s8", who);
+    const sk_extent &e = *extent;
+    sk::RmsBwdArgs a{};
+    take_span(e, &a);
+    Operands all(who, e);
+    SK_TRY(all.values("dgamma", dgamma_dev, e.c, true));
+    SK_TRY(all.values("gamma", gamma_dev, e.c, false));
+    if (!empty) {
+        if (!rstd_dev) return fail(SK_EINVAL, "%s: needs the forward pass's rstd", who);
+        SK_TRY(all.view("dy", dy, false));
+        SK_TRY(all.view("s", s, false));
+        SK_TRY(all.packed("s8", s8, false));
+        SK_TRY(all.view("dsum", dsum, false));
+        SK_TRY(all.view("dx", dx, true));
+        SK_TRY(all.values("rstd", rstd_dev, (__int128)e.n * e.plane, false));
+        const uint64_t need = dgamma_dev ? sizeof(float) * (uint64_t)sk::rms_bwd_scratch_floats(a) : 0;
+        SK_TRY(all.workspace(workspace_dev, workspace_bytes, need));
+        a.dy = take_view(dy);
+        a.s = take_view(s);
+        a.s8 = take_packed(s8);
+        a.dsum = take_view(dsum);
+        a.dx = take_view(dx);
+        a.rstd = rstd_dev;
+        a.scratch = static_cast<float *>(workspace_dev);
+        a.scratch_floats = (size_t)(need / sizeof(float));
+    }
+    SK_TRY(all.settle({dy, s, dsum}));
+    a.gamma = gamma_dev;
+    a.dgamma = dgamma_dev;
+    SK_HIP(sk::launch_rms_norm_bwd(a, static_cast<hipStream_t>(hip_stream)));
+    return SK_OK;
 }
 
 sk_status sknet_weight_gradient8_workspace(const sk_extent *extent, int64_t c_out, uint64_t *bytes)
@@ -286,34 +274,32 @@ sk_status sknet_weight_gradient8(const sk_extent *extent, int64_t c_out, const s
                                  float *db_dev, void *workspace_dev, uint64_t workspace_bytes, void *hip_stream)
 {
     const char *who = "weight_gradient8";
-    return guarded(who, [&]() -> sk_status {
-        bool empty = false;
-        SK_TRY(check_extent(who, extent, &empty));
-        if (!dy || !x || !dw_dev) return fail(SK_EINVAL, "%s: null argument", who);
-        const sk_extent &e = *extent;
-        SK_TRY(check_c_out(who, e, c_out));
-        sk::Wgrad8Args a{};
-        take_span(e, &a);
-        Operands all(who, e);
-        SK_TRY(all.values("dw", dw_dev, (__int128)c_out * e.c, true));
-        SK_TRY(all.values("db", db_dev, c_out, true));
-        if (!empty) {
-            SK_TRY(all.view("dy", dy, false, c_out));
-            SK_TRY(all.packed("x", x, false));
-            const uint64_t need = sizeof(float) * (uint64_t)sk::wgrad8_scratch_floats(a, c_out);
-            SK_TRY(all.workspace(workspace_dev, workspace_bytes, need));
-            a.dy = take_view(dy);
-            a.x = take_packed(x);
-            a.scratch = static_cast<float *>(workspace_dev);
-            a.scratch_floats = (size_t)(need / sizeof(float));
-        }
-        SK_TRY(all.settle());
-        a.c_out = c_out;
-        a.accumulate = accumulate != 0;
-        a.dw = dw_dev; a.db = db_dev;
-        SK_HIP(sk::launch_wgrad8(a, static_cast<hipStream_t>(hip_stream)));
-        return SK_OK;
-    });
+    bool empty = false;
+    SK_TRY(check_extent(who, extent, &empty));
+    if (!dy || !x || !dw_dev) return fail(SK_EINVAL, "%s: null argument", who);
+    const sk_extent &e = *extent;
+    SK_TRY(check_c_out(who, e, c_out));
+    sk::Wgrad8Args a{};
+    take_span(e, &a);
+    Operands all(who, e);
+    SK_TRY(all.values("dw", dw_dev, (__int128)c_out * e.c, true));
+    SK_TRY(all.values("db", db_dev, c_out, true));
+    if (!empty) {
+        SK_TRY(all.view("dy", dy, false, c_out));
+        SK_TRY(all.packed("x", x, false));
+        const uint64_t need = sizeof(float) * (uint64_t)sk::wgrad8_scratch_floats(a, c_out);
+        SK_TRY(all.workspace(workspace_dev, workspace_bytes, need));
+        a.dy = take_view(dy);
+        a.x = take_packed(x);
+        a.scratch = static_cast<float *>(workspace_dev);
+        a.scratch_floats = (size_t)(need / sizeof(float));
+    }
+    SK_TRY(all.settle());
+    a.c_out = c_out;
+    a.accumulate = accumulate != 0;
+    a.dw = dw_dev; a.db = db_dev;
+    SK_HIP(sk::launch_wgrad8(a, static_cast<hipStream_t>(hip_stream)));
+    return SK_OK;
 }
 
 }  // extern "C"
