@@ -6,6 +6,8 @@ namespace sk {
 namespace {
 
 // HBM bounds both.  A lane takes eight values of a line, four lanes a block, and a wave U times as many, all of them asked for before the first is used.
+// 200 x 512^2 fp32, 264 MB either way: packed in 49 us = 5.4 TB/s, unpacked in 61 = 4.3 (fp32 results are written 32 bytes a lane, in two halves; four values a lane
+// leave no gaps, and took 58 us instead of 86 alone but 75 instead of 60 behind the packing).  One thread a block: 2900 us both.
 // LONG: a wave's values are of one line, whose place it works out on the scalar unit; a line takes as many waves as it needs.  Short lines: each lane works out
 // its own.
 template <bool LONG, int U> struct Octets {
@@ -114,7 +116,7 @@ template <class F> void pick_walk(const NormSpan &s, Walk8 &w, F f)
     typedef std::integral_constant<int, 2> Two;
     typedef std::integral_constant<int, 4> Four;
     if (w.length <= kLongLine) return lines * octets < 64 * 1024 ? go(No{}, One{}) : go(No{}, Two{});
-    // no piece is left half empty
+    // so that few pieces are left half empty
     if (octets <= 64) return go(Yes{}, One{});
     if (octets <= 128 || lines * octets < 64 * 4096) return go(Yes{}, Two{});
     return go(Yes{}, Four{});

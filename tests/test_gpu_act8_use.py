@@ -165,3 +165,18 @@ def test_inputs_without_strides_of_their_own():
         got, same = B.weight_gradient8(dy.expand(wide), B.pack8(step.x, axis=1)), B.weight_gradient8(dy.expand(wide).contiguous(), B.pack8(step.x, axis=1))
         assert torch.equal(got[0], same[0]) and torch.equal(got[1], same[1])
         assert torch.equal(B.unpack8(B.pack8(r.expand(shape), axis=1)), B.unpack8(B.pack8(r, axis=1)).expand(shape))
+
+
+def test_graph_of_large_tiles():
+    from paper_1509_03371_amd import binding as B
+    x, dy = torch.randn(701, 2050, device="cuda").half(), 0.01 * torch.randn(701, 2101, device="cuda").half()
+    p = B.pack8(x, "i8")
+    want = [t.clone() for t in B.weight_gradient8(dy, p)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = B.weight_gradient8(dy, p)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        got[0].zero_()
