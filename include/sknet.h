@@ -517,8 +517,9 @@ sk_status sknet_rms_norm_backward(const sk_extent *extent, const sk_view *dy, co
 /* Weight gradient of an inner product, or of a 1x1 convolution, over inputs held in 8 bits: with the extent's n * plane positions q and c input channels k,
  *   dw[o][k] = sum_q dy[q][o] x[q][k],  db[o] = sum_q dy[q][o]      (accumulate != 0: added to what dw and db hold)
  * dy: of the extent's type and order with c_out channels in the place of c.  dw_dev: DEVICE [c_out][c], db_dev: DEVICE [c_out] or NULL.  Products are exact:
- * dy goes to the matrix unit whole (bf16) or as two (fp16) or three (fp32) bf16 terms that add up to it, x as it is; sums are fp32, in an order
- * that the sizes alone settle: equal calls give equal bits.  workspace_dev as above, from sknet_weight_gradient8_workspace.
+ * dy goes to the matrix unit whole (bf16) or as two (fp16) or three (fp32) bf16 terms that add up to it (but for parts below 2^-126), x as it is; sums are fp32, in an order
+ * that the sizes alone settle: equal calls give equal bits.  Lines are read in pieces of 32 values: what lies between the lines of dy and of x's codes is read with
+ * them and left out of account, so all memory from the first to the last element of each must be readable.  workspace_dev as above, from sknet_weight_gradient8_workspace.
  * Limits (SK_EUNSUPPORTED): those of an extent, c_out <= 2^27, c * c_out <= 2^40. */
 sk_status sknet_weight_gradient8_workspace(const sk_extent *extent, int64_t c_out, uint64_t *bytes);
 sk_status sknet_weight_gradient8(const sk_extent *extent, int64_t c_out, const sk_view *dy, const sk_packed *x, int32_t accumulate, float *dw_dev,
