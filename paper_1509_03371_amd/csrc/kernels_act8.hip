@@ -41,7 +41,8 @@ template <bool LONG, int U> struct Octets {
     __device__ __forceinline__ bool there(const At &p) const { return LONG ? 8 * p.o < w.length : p.b < a.n; }
 };
 
-template <int DT, int CODE, bool LONG, int U> __global__ __launch_bounds__(256) void pack8_kernel(Pack8Args a, Walk8 w)
+// LANES that hold a block: four, or one where lines have eight values at most
+template <int DT, int CODE, bool LONG, int U, int LANES> __global__ __launch_bounds__(256) void pack8_kernel(Pack8Args a, Walk8 w)
 {
     const long step = gridDim.x * 4L;
     for (long wave = neighbour() * 4L + uniform(threadIdx.x >> 6); wave < w.waves; wave += step) {
@@ -62,7 +63,7 @@ template <int DT, int CODE, bool LONG, int U> __global__ __launch_bounds__(256) 
             for (int j = 0; j < 8; ++j) f[j] = x[u][j];
             uint8_t *codes = a.packed.codes + p.b * a.packed.sn + (w.maps ? p.k * a.packed.sc : 0) + 8 * p.o;
             uint8_t *scale = a.packed.scales + p.b * a.packed.ssn + (w.maps ? p.k * a.packed.ssc : 0) + p.o / 4;
-            put_octet<DT, CODE, 4>(f, left[u], codes, p.o % 4 == 0 ? scale : nullptr);
+            put_octet<DT, CODE, LANES>(f, left[u], codes, p.o % 4 == 0 ? scale : nullptr);
         }
     }
 }
@@ -93,13 +94,14 @@ template <int DT, int CODE, bool LONG, int U> __global__ __launch_bounds__(256) 
 
 constexpr long kLongLine = 256;
 
-// f(LONG, U), and the walk
+// f(LONG, U, LANES), and the walk
 template <class F> void pick_walk(const NormSpan &s, Walk8 &w, F f)
 {
     w.maps = s.layout == MAPS;
     w.length = w.maps ? s.plane : s.c;
-    const long lines = w.maps ? s.n * s.c : s.n, octets = 4 * blocks_of(w.length);
-    auto go = [&](auto is_long, auto u) {
+    // (lines of at most eight: one lane each.  1551889 rows of four fp16 there and back: 26 us, with four lanes a line 71.)
+    const long lines = w.maps ? s.n * s.c : s.n, octets = w.length <= 8 ? 1 : 4 * blocks_of(w.length);
+    auto go = [&](auto is_long, auto u, auto lanes) {
         if (is_long()) {
             w.pieces = (octets + 64 * u() - 1) / (64 * u());
             w.waves = lines * w.pieces;
@@ -108,18 +110,20 @@ template <class F> void pick_walk(const NormSpan &s, Walk8 &w, F f)
             w.channels = Divisor8(s.c);
             w.waves = (lines * octets + 64 * u() - 1) / (64 * u());
         }
-        f(is_long, u);
+        f(is_long, u, lanes);
     };
     typedef std::true_type Yes;
     typedef std::false_type No;
     typedef std::integral_constant<int, 1> One;
     typedef std::integral_constant<int, 2> Two;
     typedef std::integral_constant<int, 4> Four;
-    if (w.length <= kLongLine) return lines * octets < 64 * 1024 ? go(No{}, One{}) : go(No{}, Two{});
+    const bool few = lines * octets < 64 * 1024;
+    if (w.length <= 8) return few ? go(No{}, One{}, One{}) : go(No{}, Two{}, One{});
+    if (w.length <= kLongLine) return few ? go(No{}, One{}, Four{}) : go(No{}, Two{}, Four{});
     // so that few pieces are left half empty
-    if (octets <= 64) return go(Yes{}, One{});
-    if (octets <= 128 || lines * octets < 64 * 4096) return go(Yes{}, Two{});
-    return go(Yes{}, Four{});
+    if (octets <= 64) return go(Yes{}, One{}, Four{});
+    if (octets <= 128 || lines * octets < 64 * 4096) return go(Yes{}, Two{}, Four{});
+    return go(Yes{}, Four{}, Four{});
 }
 
 template <class F> void pick_dtype(int dtype, F f)
@@ -134,9 +138,9 @@ template <class F> void pick_dtype(int dtype, F f)
 hipError_t launch_pack8(const Pack8Args &a, hipStream_t stream)
 {
     Walk8 w;
-    pick_walk(a, w, [&](auto is_long, auto u) {
+    pick_walk(a, w, [&](auto is_long, auto u, auto lanes) {
         pick_dtype(a.dtype, [&](auto dt) {
-            pick_code(a.packed.code, [&](auto code) { pack8_kernel<dt(), code(), is_long(), u()><<<norm_blocks(w.waves, 4), 256, 0, stream>>>(a, w); });
+            pick_code(a.packed.code, [&](auto code) { pack8_kernel<dt(), code(), is_long(), u(), lanes()><<<norm_blocks(w.waves, 4), 256, 0, stream>>>(a, w); });
         });
     });
     return hipGetLastError();
@@ -145,7 +149,7 @@ hipError_t launch_pack8(const Pack8Args &a, hipStream_t stream)
 hipError_t launch_unpack8(const Pack8Args &a, hipStream_t stream)
 {
     Walk8 w;
-    pick_walk(a, w, [&](auto is_long, auto u) {
+    pick_walk(a, w, [&](auto is_long, auto u, auto) {
         pick_dtype(a.dtype, [&](auto dt) {
             pick_code(a.packed.code, [&](auto code) { unpack8_kernel<dt(), code(), is_long(), u()><<<norm_blocks(w.waves, 4), 256, 0, stream>>>(a, w); });
         });

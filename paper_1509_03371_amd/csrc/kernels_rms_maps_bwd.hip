@@ -241,7 +241,9 @@ template <int DT, bool HELD> __global__ __launch_bounds__(256) void rms_deep_dga
 int copies_of(const NormSpan &s, int p, int v, int k, int threads)
 {
     if (!k) return (int)std::min<long>((s.n * s.plane + 1023) / 1024, 64);
-    return (int)std::min<long>(s.n * tiles_per_image(s, p * v), std::max(1, 256 * 1024 / threads));
+    // up to four tiles are one workgroup's: no second launch, whose 4 us are two tiles' time
+    const long tiles = s.n * tiles_per_image(s, p * v);
+    return tiles <= 4 ? 1 : (int)std::min<long>(tiles, std::max(1, 256 * 1024 / threads));
 }
 
 }  // namespace

@@ -494,7 +494,7 @@ int rms_rows_bwd_copies(const NormSpan &s)
     if (takes_roles(s)) return copies;
     pick_rows_bwd(s.c, false, [&](auto g, auto, auto t) {
         const long rounds = (s.n + t() / g() - 1) / (t() / g());
-        copies = (int)std::min<long>(rounds, 256 * 1024 / t());
+        copies = rounds <= 4 && s.c <= 8 ? 1 : (int)std::min<long>(rounds, 256 * 1024 / t());       // (rows of up to eight channels have no roles)
     });
     return copies;
 }
