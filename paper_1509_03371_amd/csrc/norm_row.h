@@ -65,12 +65,15 @@ template <int DT, int G> struct Row {
     // row: the first of the wave's
     __device__ __forceinline__ src_t from(const NormView &v, long row) const { return static_cast<src_t>(v.p) + S * row * v.sn; }
     __device__ __forceinline__ uint32_t offset(const NormView &v) const { return G < 64 ? (uint32_t)sub * (uint32_t)(S * v.sn) : 0; }
-    __device__ __forceinline__ void store(const NormView &v, long row, int k, const float (&f)[8]) const
+    // PLAIN: as data that may be read again soon
+    template <bool PLAIN = false> __device__ __forceinline__ void store(const NormView &v, long row, int k, const float (&f)[8]) const
     {
         const int left = c - channel(k);
         const dst_t p = static_cast<dst_t>(v.p) + S * row * v.sn;
         const uint32_t off = offset(v) + S * channel(k);
-        if (left >= 8) {
+        if (PLAIN && left >= 8) {
+            *reinterpret_cast<line_t<DT, 8> *>(p + off) = packed<DT, 8>(f);
+        } else if (left >= 8) {
             store_at<DT, 8>(p, off, f);
         } else if (left > 0) {                          // c % 8 elements, by four, two and one
             const int r = c % 8;
