@@ -351,7 +351,7 @@ class _Operator:
     def place(self, order=None, **tensors):
         """Find the order that the tensors have in common (order: that one alone); returns the extent, and their views by name (None for None)."""
         x = self.x
-        shape, dtype, device = x.shape, x.dtype, self.device
+        shape, dtype, device = x.shape, x.dtype, x.get_device()
         strides, places = [x.stride()], []
         for name, t in tensors.items():
             if t is None:
@@ -359,8 +359,8 @@ class _Operator:
             elif t is x:
                 places.append(0)
             else:
-                if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype):
-                    raise TypeError("%s must be a tensor of %s on %s" % (name, dtype, device))
+                if not (isinstance(t, torch.Tensor) and t.get_device() == device and t.dtype == dtype):
+                    raise TypeError("%s must be a tensor of %s on %s" % (name, dtype, self.device))
                 if t.shape != shape:
                     raise ValueError("%s has shape %s instead of %s" % (name, tuple(t.shape), tuple(shape)))
                 places.append(len(strides))
@@ -380,7 +380,7 @@ class _Operator:
         """DEVICE pointer of `count` fp32 values, None for None."""
         if t is None:
             return None
-        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == torch.float32 and t.is_contiguous()):
+        if not (isinstance(t, torch.Tensor) and t.get_device() == self.device.index and t.dtype == torch.float32 and t.is_contiguous()):
             raise TypeError("%s must be a contiguous tensor of torch.float32 on %s" % (name, self.device))
         if t.numel() != count:
             raise ValueError("%s has %d values instead of %d" % (name, t.numel(), count))
@@ -468,16 +468,17 @@ class Packed:
 
     def __init__(self, codes, scales, code="e4m3", axis=-1):
         for t, name in ((codes, "codes"), (scales, "scales")):
-            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.uint8):
+            if not (isinstance(t, torch.Tensor) and t.dtype == torch.uint8 and t.is_cuda):
                 raise TypeError("%s must be a CUDA tensor of torch.uint8" % name)
-        if scales.device != codes.device:
+        if scales.get_device() != codes.get_device():
             raise TypeError("scales must be on %s" % (codes.device,))
         if code not in CODES:
             raise ValueError("code must be one of %s" % sorted(CODES))
-        if not -codes.dim() <= axis < codes.dim():
+        shape = codes.shape
+        if not -len(shape) <= axis < len(shape):
             raise ValueError("codes has no axis %d" % axis)
-        self.codes, self.scales, self.code, self.axis = codes, scales, code, axis % codes.dim()
-        self.order, strides = _packed_order(codes.shape, codes.stride(), self.axis, scales.shape, scales.stride())
+        self.codes, self.scales, self.code, self.axis = codes, scales, code, axis % len(shape)
+        self.order, strides = _packed_order(shape, codes.stride(), self.axis, scales.shape, scales.stride())
         self.view = SkPacked(CODES[code], codes.data_ptr(), scales.data_ptr(), *strides)
 
     @classmethod
