@@ -194,7 +194,7 @@ template <bool IS_ROWS> __device__ __forceinline__ bf16x8 fragment(const char *l
 
 // A workgroup takes TM x TN weights and a share of the positions, KS at a time: its threads load 32 values of a line each (of x a block with its scale), a step
 // ahead, widen them on their way into LDS, and its waves multiply, a part of the tile each.  db comes out of the same fragments, times ones.
-// 16384 rows, 2048 x 4096 weights, 275 GFLOP: bf16 and e4m3 341 us = 0.81 PFLOP/s, int8 402 (a library product of bf16 tensors 231: 1.19).  Waves that multiply go first
+// 16384 rows, 2048 x 4096 weights, 275 GFLOP: bf16 and e4m3 346 us = 0.80 PFLOP/s, int8 396 (a library product of bf16 tensors 231: 1.19).  Waves that multiply go first
 // (s_setprio): 398 without.  What is left waits for the loads of a step, of which one is under way: three workgroups a CU at 160 registers cover for one another, two (240
 // registers) take 483 us, steps of 32 positions 464, 256 x 128 tiles of four waves with two steps under way 668.  fp16 and fp32 have two and three products for each
 // load, and there BIG tiles pay: 8192 rows, 2048 x 2048 fp16 184 us and 253 with small ones (bf16 424 and 398).
@@ -220,47 +220,43 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN, bool BIG> __global__ _
     Unit<B> dy;
     Unit<1> x;
     uint32_t scale = 0;
-    auto fetch = [&](long step) {
-        if constexpr (IS_ROWS) {
-            const long qm = step * KS + um / (TM / 32), qn = step * KS + un / (TN / 32);
-            const long om = m0 + 32 * (um % (TM / 32)), kn = n0 + 32 * (un % (TN / 32));
-            if (has_m) {
-                if (qm < a.n && om < a.c_out) dy.load(static_cast<const char *>(a.dy.p), (qm * a.dy.sn + om) * B, a.dy_end, (int)std::min<long>(32, a.c_out - om));
-                else dy.clear();
+    // Where they lie: a part of the thread's own that stays, and one of the step's that all share and the scalar unit keeps.
+    const long om = IS_ROWS ? m0 + 32 * (um % (TM / 32)) : std::min(m0 + um / per, a.c_out - 1);
+    const long kn = IS_ROWS ? n0 + 32 * (un % (TN / 32)) : std::min<long>(n0 + un / per, a.c - 1);
+    const int row_m = um / (TM / 32), row_n = un / (TN / 32), px_m = 32 * (um % per), px_n = 32 * (un % per);
+    const long at_dy = B * (IS_ROWS ? row_m * a.dy.sn + om : om * a.dy.sc + px_m);
+    const long at_x = IS_ROWS ? row_n * a.x.sn + kn : kn * a.x.sc + px_n, at_scale = IS_ROWS ? row_n * a.x.ssn + kn / 32 : kn * a.x.ssc + px_n / 32;
+    const long first = a.steps * split / a.splits, last = a.steps * (split + 1) / a.splits;
+    long b = IS_ROWS ? 0 : first / a.plane_steps, q0 = IS_ROWS ? first * KS : (first - b * a.plane_steps) * KS;      // image; row or pixel
+    auto fetch = [&] {                                  // the next step's
+        const long left = (IS_ROWS ? a.n : a.plane) - q0;
+        const long dy0 = IS_ROWS ? q0 * a.dy.sn : b * a.dy.sn + q0, x0 = IS_ROWS ? q0 * a.x.sn : b * a.x.sn + q0;
+        const long scale0 = IS_ROWS ? q0 * a.x.ssn : b * a.x.ssn + q0 / 32;
+        const int some = left < KS ? (int)left : KS;    // rows, or pixels, of the step
+        if (has_m) {
+            const int count = IS_ROWS ? (row_m < some && om < a.c_out ? (int)std::min<long>(32, a.c_out - om) : 0) : std::min(32, some - px_m);
+            if (count > 0) {
+                dy.load(static_cast<const char *>(a.dy.p), B * dy0 + at_dy, a.dy_end, count);
+                if (!IS_ROWS && count < 32) dy.keep(count);
+            } else {
+                dy.clear();
             }
-            if (has_n) {
-                if (qn < a.n && kn < a.c) {
-                    x.load(reinterpret_cast<const char *>(a.x.codes), qn * a.x.sn + kn, a.codes_end, (int)std::min<long>(32, a.c - kn));
-                    scale = a.x.scales[qn * a.x.ssn + kn / 32];
-                } else {
-                    x.clear();
-                    scale = 127;
-                }
+        }
+        if (has_n) {
+            const int count = IS_ROWS ? (row_n < some && kn < a.c ? (int)std::min<long>(32, a.c - kn) : 0) : std::min(32, some - px_n);
+            if (count > 0) {
+                x.load(reinterpret_cast<const char *>(a.x.codes), x0 + at_x, a.codes_end, count);
+                if (!IS_ROWS && count < 32) x.keep(count);
+                scale = a.x.scales[scale0 + at_scale];
+            } else {
+                x.clear();
+                scale = 127;
             }
-        } else {
-            const long b = step / a.plane_steps, first = (step - b * a.plane_steps) * KS;
-            const long om = std::min(m0 + um / per, a.c_out - 1), kn = std::min<long>(n0 + un / per, a.c - 1);
-            const long pm = first + 32 * (um % per), pn = first + 32 * (un % per);
-            if (has_m) {
-                const int count = (int)std::min<long>(32, a.plane - pm);
-                if (count > 0) {
-                    dy.load(static_cast<const char *>(a.dy.p), (b * a.dy.sn + om * a.dy.sc + pm) * B, a.dy_end, count);
-                    if (count < 32) dy.keep(count);
-                } else {
-                    dy.clear();
-                }
-            }
-            if (has_n) {
-                const int count = (int)std::min<long>(32, a.plane - pn);
-                if (count > 0) {
-                    x.load(reinterpret_cast<const char *>(a.x.codes), b * a.x.sn + kn * a.x.sc + pn, a.codes_end, count);
-                    if (count < 32) x.keep(count);
-                    scale = a.x.scales[b * a.x.ssn + kn * a.x.ssc + pn / 32];
-                } else {
-                    x.clear();
-                    scale = 127;
-                }
-            }
+        }
+        q0 += KS;
+        if (!IS_ROWS && q0 >= a.plane) {
+            q0 = 0;
+            ++b;
         }
     };
     auto put = [&](char *lds) {
@@ -309,16 +305,15 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN, bool BIG> __global__ _
                 }
         }
     };
-    const long first = a.steps * split / a.splits, last = a.steps * (split + 1) / a.splits;
-    fetch(first);
+    fetch();
     if constexpr (BIG) {
         put(smem);
-        if (first + 1 < last) fetch(first + 1);
+        if (first + 1 < last) fetch();
         int now = 0;
         for (long step = first; step < last; ++step) {
             __syncthreads();                            // this step is in LDS, and the one before has been read
             if (step + 1 < last) put(smem + (now ^ 1) * buffer);
-            if (step + 2 < last) fetch(step + 2);
+            if (step + 2 < last) fetch();
             __builtin_amdgcn_s_setprio(1);
             multiply(smem + now * buffer);
             __builtin_amdgcn_s_setprio(0);
@@ -329,7 +324,7 @@ template <int DT, int CODE, bool IS_ROWS, int TM, int TN, bool BIG> __global__ _
             __syncthreads();                            // the step before has been read
             put(smem);
             __syncthreads();
-            if (step + 1 < last) fetch(step + 1);
+            if (step + 1 < last) fetch();
             __builtin_amdgcn_s_setprio(1);
             multiply(smem);
             __builtin_amdgcn_s_setprio(0);
