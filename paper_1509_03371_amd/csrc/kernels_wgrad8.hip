@@ -194,7 +194,7 @@ template <bool IS_ROWS> __device__ __forceinline__ bf16x8 fragment(const char *l
 
 // A workgroup takes TM x TN weights and a share of the positions, KS at a time: its threads load 32 values of a line each (of x a block with its scale), a step
 // ahead, widen them on their way into LDS, and its waves multiply, a part of the tile each.  db comes out of the same fragments, times ones.
-// 16384 rows, 2048 x 4096 weights, 275 GFLOP: bf16 and e4m3 346 us = 0.80 PFLOP/s, int8 396 (a library product of bf16 tensors 231: 1.19).  Waves that multiply go first
+// 16384 rows, 2048 x 4096 weights, 275 GFLOP: bf16 and e4m3 350 us = 0.79 PFLOP/s, int8 396 (a library product of bf16 tensors 231: 1.19).  Waves that multiply go first
 // (s_setprio): 398 without.  What is left waits for the loads of a step, of which one is under way: three workgroups a CU at 160 registers cover for one another, two (240
 // registers) take 483 us, steps of 32 positions 464, 256 x 128 tiles of four waves with two steps under way 668.  fp16 and fp32 have two and three products for each
 // load, and there BIG tiles pay: 8192 rows, 2048 x 2048 fp16 184 us and 253 with small ones (bf16 424 and 398).
