@@ -180,3 +180,27 @@ def test_graph_of_large_tiles():
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         got[0].zero_()
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("more", [1, 2, 3])
+def test_planes_that_end_behind_a_tiles_first_pixels(more, kind):
+    """The last tile of a plane holds one to three pixels: its first lane reads from the tile in front of it."""
+    from paper_1509_03371_amd import binding as B
+    for c, tile in ((9, 256), (48, 128), (100, 64), (200, 32), (600, 32), (1100, 32)):
+        shape = (2, c, 2 * tile + more)
+        x, r, gamma, _, dy, _ = inputs(shape, kind, 13, 0.3)
+        x, r, dy, gd = place(x, kind), place(r, kind), place(dy, kind), torch.from_numpy(gamma).cuda()
+        sum8 = B.Packed.like(x, "i8", axis=1)
+        y, s, rstd = B.rms_norm(x, gd, axis=1, residual=r, sum8=sum8)
+        rs = to64(x) + to64(r)
+        es = 2.0 ** -24 * np.abs(rs)
+        ry, rr, ey, er = norm_bounds(rs, es, gamma, 1e-5)
+        close(y, ry, rounded(ry, kind, ey), "y")
+        close(rstd, rr, er, "rstd")
+        held(sum8.codes, sum8.scales, "i8", kind, rs, es, "sum8")
+        for source in (s, sum8):
+            dx, dgamma = B.rms_norm_backward(dy, source, rstd, gd, axis=1, dsum=r)
+            t, rg, et, eg = bwd_bounds(to64(dy), to64(s if source is s else B.unpack8(sum8)), to64(rstd), gamma, to64(r))
+            close(dx, t, rounded(t, kind, et), "dx")
+            close(dgamma, rg, eg, "dgamma")
