@@ -86,7 +86,7 @@ template <int DT, int P, int V, int K, int T> __global__ __launch_bounds__(T) vo
         t.total(q, part, half);
         float rstd[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) rstd[i] = 1.f / sqrtf(q[i] / (float)a.c + a.eps);
+        for (int i = 0; i < V; ++i) rstd[i] = inverse_root(q[i] / (float)a.c + a.eps);
         if (K) {
 #pragma unroll
             for (int k = 0; k < K; ++k) put_maps(t, a, t.octet0 + k * t.octets, rstd, s[k]);

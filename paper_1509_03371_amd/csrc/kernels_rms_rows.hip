@@ -81,7 +81,7 @@ template <int DT, int G, int K, int T> __global__ __launch_bounds__(T) void rms_
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j) q += s[k][j] * s[k][j];             // channels behind the last are zeros
-        const float rstd = 1.f / sqrtf(total(q) / (float)a.c + a.eps);
+        const float rstd = inverse_root(total(q) / (float)a.c + a.eps);
 #pragma unroll
         for (int k = 0; k < K; ++k) put_row(r, a, row0, k, exact, rstd, s[k]);
         if (r.lane == 0 && a.rstd) a.rstd[row] = rstd;
@@ -118,7 +118,7 @@ template <int DT> __global__ __launch_bounds__(1024) void rms_long_rows_kernel(R
             for (int j = 0; j < 8; ++j) t += s[j] * s[j];
             q += t;
         }
-        const float rstd = 1.f / sqrtf(total(q) / (float)a.c + a.eps);
+        const float rstd = inverse_root(total(q) / (float)a.c + a.eps);
         for (int k = 0; k < K; ++k) {
             values(k);
             put_row(r, a, row, k, false, rstd, s);

@@ -25,6 +25,15 @@ __device__ __forceinline__ void held_octet(const PackedView &v, const uint32_t (
     else octet_of_codes<I8>(c, byte, f);
 }
 
+// 1 / sqrt(v), rounded once: the root and the division, rounded each, are up to three half steps off (more than one for a quarter of all v), and what they are off goes into every
+// value of the position.  r = (1 / sqrt v)(1 + d) has 1 - v r^2 = -2 d but for d^2, taken from the whole product v r = h + l.  Infinite v: 0.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = 1.f / sqrtf(v), h = v * r, l = fmaf(v, r, -h);
+    const float e = fmaf(-h, r, 1.f) - l * r;
+    return r > 0.f ? fmaf(0.5f * r, e, r) : r;
+}
+
 // dgamma from the `copies` copies of its sums, each of c rounded up to 4
 __host__ __device__ inline long rms_copy_floats(long c) { return (c + 3) / 4 * 4; }
 hipError_t launch_rms_reduce(const float *scratch, int copies, float *dgamma, int c, hipStream_t stream);
