@@ -464,22 +464,30 @@ def layer_norm_backward(dy, s, mean, rstd, gamma=None, axis=-1, dsum=None, p=0.0
 class Packed:
     """A tensor in 8 bits, in blocks of 32 neighbours with a scale each.  codes: uint8 tensor of the tensor's sizes, with the channels on `axis`, as
     rows or as maps; scales: uint8 tensor of [positions, blocks of a row] or [images, channels, blocks of a map], which tells the two apart.
-    code: "e4m3" or "i8"."""
+    code: "e4m3" or "i8".  The tensors are looked at anew by every call: they may be replaced, moved to another memory and back, copied or pickled in between."""
 
     def __init__(self, codes, scales, code="e4m3", axis=-1):
-        for t, name in ((codes, "codes"), (scales, "scales")):
-            if not (isinstance(t, torch.Tensor) and t.dtype == torch.uint8 and t.is_cuda):
-                raise TypeError("%s must be a CUDA tensor of torch.uint8" % name)
-        if scales.get_device() != codes.get_device():
-            raise TypeError("scales must be on %s" % (codes.device,))
-        if code not in CODES:
+        self.codes, self.scales, self.code = codes, scales, code
+        self.axis = axis + codes.dim() if axis < 0 and isinstance(codes, torch.Tensor) else axis
+        self.place()
+
+    def place(self):
+        """(order, strides) of the tensors as they are now."""
+        codes, scales, byte = self.codes, self.scales, torch.uint8
+        if not (isinstance(codes, torch.Tensor) and codes.dtype == byte and codes.is_cuda):
+            raise TypeError("codes must be a CUDA tensor of torch.uint8")
+        if not (isinstance(scales, torch.Tensor) and scales.dtype == byte and scales.get_device() == codes.get_device()):
+            raise TypeError("scales must be a tensor of torch.uint8 on %s" % (codes.device,))
+        if self.code not in CODES:
             raise ValueError("code must be one of %s" % sorted(CODES))
-        shape = codes.shape
-        if not -len(shape) <= axis < len(shape):
-            raise ValueError("codes has no axis %d" % axis)
-        self.codes, self.scales, self.code, self.axis = codes, scales, code, axis % len(shape)
-        self.order, strides = _packed_order(shape, codes.stride(), self.axis, scales.shape, scales.stride())
-        self.view = SkPacked(CODES[code], codes.data_ptr(), scales.data_ptr(), *strides)
+        if not 0 <= self.axis < codes.dim():
+            raise ValueError("codes has no axis %d" % self.axis)
+        return _packed_order(codes.shape, codes.stride(), self.axis, scales.shape, scales.stride())
+
+    @property
+    def order(self):
+        """(layout, n, c, plane): how the codes lie."""
+        return self.place()[0]
 
     @classmethod
     def like(cls, x, code="e4m3", axis=-1):
@@ -513,24 +521,25 @@ def _packed_order(shape, strides, axis, scales_shape, scales_strides):
 
 
 def _packed(op, p, name):
-    """Reference to a Packed of the operator's sizes, None for None."""
+    """Order of a Packed of the operator's sizes and reference to it, None for None."""
     if p is None:
-        return None
+        return None, None
     if not isinstance(p, Packed):
         raise TypeError("%s must be a Packed" % name)
-    if p.codes.device != op.device:
+    order, strides = p.place()
+    if p.codes.get_device() != op.device.index:
         raise TypeError("%s must be on %s" % (name, op.device))
     if p.codes.shape != op.x.shape or p.axis != op.axis:
         raise ValueError("%s has shape %s and channels on axis %d instead of %s and %d" % (name, tuple(p.codes.shape), p.axis, tuple(op.x.shape), op.axis))
-    return C.byref(p.view)
+    return order, C.byref(SkPacked(CODES[p.code], p.codes.data_ptr(), p.scales.data_ptr(), *strides))
 
 
-def _one_order(*packed):
-    """The order of those that are there; theirs have to agree."""
-    orders = {p.order for p in packed if isinstance(p, Packed)}
-    if len(orders) > 1:
-        raise ValueError("the tensors in 8 bits are in unlike orders: %s" % sorted(orders))
-    return orders.pop() if orders else None
+def _one_order(*orders):
+    """The order of those that are there; they have to agree."""
+    there = {o for o in orders if o is not None}
+    if len(there) > 1:
+        raise ValueError("the tensors in 8 bits are in unlike orders: %s" % sorted(there))
+    return there.pop() if there else None
 
 
 def pack8(x, code="e4m3", axis=-1, out=None, stream=None):
@@ -538,8 +547,8 @@ def pack8(x, code="e4m3", axis=-1, out=None, stream=None):
     with _Operator(x, axis, "x", stream) as op:
         if out is None:
             out = Packed.like(x, code, axis)
-        packed = _packed(op, out, "out")
-        xv, = op.place(out.order)
+        order, packed = _packed(op, out, "out")
+        xv, = op.place(order)
         _check(lib.sknet_pack8(C.byref(op.extent), xv, packed, op.stream))
     return out
 
@@ -549,6 +558,7 @@ def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
     if not isinstance(packed, Packed):
         raise TypeError("packed must be a Packed")
     if out is None:
+        packed.place()
         device = packed.codes.device
         if dtype not in _OP_TYPES:
             raise TypeError("dtype must be one of %s" % sorted(map(str, _OP_TYPES)))
@@ -557,8 +567,8 @@ def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             out = torch.empty_like(packed.codes, dtype=dtype)
     with _Operator(out, packed.axis, "out", stream) as op:
-        ref = _packed(op, packed, "packed")
-        yv, = op.place(packed.order)
+        order, ref = _packed(op, packed, "packed")
+        yv, = op.place(order)
         _check(lib.sknet_unpack8(C.byref(op.extent), ref, yv, op.stream))
     return out
 
@@ -574,10 +584,11 @@ def rms_norm(x, gamma=None, eps=1e-5, axis=-1, residual=None, out=None, sum_out=
             sum_out = op.output()
         if rstd is None:
             rstd = torch.empty(x.shape[:op.axis] + x.shape[op.axis + 1:], dtype=torch.float32, device=x.device)
-        packed = _packed(op, sum8, "sum8"), _packed(op, y8, "y8")
-        xv, rv, sv, yv = op.place(_one_order(sum8, y8), residual=residual, sum_out=None if sum_out is False else sum_out, out=None if out is False else out)
+        sum_order, sum_ref = _packed(op, sum8, "sum8")
+        y_order, y_ref = _packed(op, y8, "y8")
+        xv, rv, sv, yv = op.place(_one_order(sum_order, y_order), residual=residual, sum_out=None if sum_out is False else sum_out, out=None if out is False else out)
         _, n, c, plane = op.order
-        _check(lib.sknet_rms_norm(C.byref(op.extent), xv, rv, op.values(gamma, c, "gamma"), eps, sv, packed[0], yv, packed[1],
+        _check(lib.sknet_rms_norm(C.byref(op.extent), xv, rv, op.values(gamma, c, "gamma"), eps, sv, sum_ref, yv, y_ref,
                                   op.values(rstd, n * plane, "rstd"), op.stream))
     return None if out is False else out, None if sum_out is False else x if sum_out is None else sum_out, rstd
 
@@ -596,8 +607,8 @@ def rms_norm_backward(dy, s, rstd, gamma=None, axis=-1, dsum=None, parameters=Tr
         if dx is None:
             dx = op.output()
         held = s if isinstance(s, Packed) else None
-        ref = _packed(op, held, "s")
-        dyv, sv, dsv, dxv = op.place(_one_order(held), s=None if held else s, dsum=dsum, dx=dx)
+        order, ref = _packed(op, held, "s")
+        dyv, sv, dsv, dxv = op.place(order, s=None if held else s, dsum=dsum, dx=dx)
         _, n, c, plane = op.order
         workspace, bytes_ = None, 0
         if parameters:
@@ -626,9 +637,9 @@ def weight_gradient8(dy, x, accumulate=False, bias=True, dw=None, db=None, strea
     if not isinstance(x, Packed):
         raise TypeError("x must be a Packed")
     with _Operator(dy, x.axis, "dy", stream) as op:
-        if x.codes.device != op.device:
+        (layout, n, c, plane), strides = x.place()
+        if x.codes.get_device() != op.device.index:
             raise TypeError("x must be on %s" % (op.device,))
-        layout, n, c, plane = x.order
         c_out = dy.shape[op.axis] if dy.dim() == x.codes.dim() else -1
         if dy.shape != x.codes.shape[:x.axis] + (c_out,) + x.codes.shape[x.axis + 1:]:
             raise ValueError("dy has shape %s, x %s with channels on axis %d" % (tuple(dy.shape), tuple(x.codes.shape), x.axis))
@@ -638,6 +649,7 @@ def weight_gradient8(dy, x, accumulate=False, bias=True, dw=None, db=None, strea
             raise ValueError("bias=False leaves no gradient to write")
         dyv, = op.place((layout, n, c_out, plane))
         extent = SkExtent(op.extent.dtype, layout, n, c, plane)
+        packed = SkPacked(CODES[x.code], x.codes.data_ptr(), x.scales.data_ptr(), *strides)
         if dw is None:
             dw = torch.empty((c_out, c), dtype=torch.float32, device=op.device)
         elif tuple(dw.shape) != (c_out, c):
@@ -646,7 +658,7 @@ def weight_gradient8(dy, x, accumulate=False, bias=True, dw=None, db=None, strea
             db = torch.empty(c_out, dtype=torch.float32, device=op.device)
         bytes_ = _gradient8_workspace(extent.dtype, layout, n, c, plane, c_out)
         workspace = torch.empty(bytes_, dtype=torch.uint8, device=op.device) if bytes_ else None
-        _check(lib.sknet_weight_gradient8(C.byref(extent), c_out, dyv, C.byref(x.view), int(accumulate), op.values(dw, c_out * c, "dw"),
+        _check(lib.sknet_weight_gradient8(C.byref(extent), c_out, dyv, C.byref(packed), int(accumulate), op.values(dw, c_out * c, "dw"),
                                           op.values(db, c_out, "db"), None if workspace is None else workspace.data_ptr(), bytes_, op.stream))
     return dw, db
 
