@@ -474,10 +474,10 @@ sk_status sknet_layer_norm_backward(const sk_extent *extent, const sk_view *dy, 
  * block's largest magnitude is at most Q 2^k.  A code is value / 2^k rounded to the nearest, ties to even:
  *   SK_E4M3: Q = 448; sign, 4 bits of exponent (bias 7), 3 of mantissa, no infinities, 0x7F (and 0xFF) = NaN;
  *   SK_I8  : Q = 127; two's complement of -127 .. 127, -128 = NaN.
- * So a value is off by at most half a step: SK_E4M3 2^-4 of itself or 2^(k-10) (values below 2^(k-6)), SK_I8 2^(k-1) < largest / 126.  Infinite and NaN elements
- * become NaN and leave the others of their block as they are: the largest is taken over the finite ones.  Magnitudes beyond the largest that
- * a code can stand for in the extent's dtype are limited to it (SK_F16: 61440 and 65024, else 1.875 * 2^127 and 127 * 2^120), so that finite values stay finite.
- * What a code stands for is exact in bf16.
+ * Magnitudes beyond the largest that a code can stand for in the extent's dtype are first limited to it (SK_F16: 61440 and 65024, else 1.875 * 2^127 and 127 * 2^120), so that
+ * finite values stay finite.  All others are off by at most half a step: SK_E4M3 2^-4 of themselves or 2^(k-10) (values below 2^(k-6)), SK_I8 2^(k-1), which is less than
+ * largest / 126 where k is more than -117.  Infinite and NaN elements become NaN and leave the others of their block as they are: the largest is taken over the
+ * finite ones.  What a code stands for is exact in bf16.
  *
  * codes: element (position, channel) is the byte at the place that an sk_view of these strides gives it.  scales: of the line of row b, or of map k
  * of image b, at b*scale_stride_n (+ k*scale_stride_c), one byte for each block, side by side.  Lines of a result must not overlap (SK_ESHAPE).  scales
@@ -500,7 +500,8 @@ sk_status sknet_unpack8(const sk_extent *extent, const sk_packed *packed, const 
 
 /* s = x + residual (residual: NULL leaves it out);  per position: rstd = 1 / sqrt(sum_k s^2 / c + eps);  y = s * rstd * gamma.
  * gamma_dev: DEVICE [c], NULL = 1.  Results, each may be NULL: sum and sum8 receive s, y and y8 receive y, in the extent's type and in 8 bits, all made from the
- * fp32 values, rounded once; rstd_dev: DEVICE [n*plane].  y or sum may be x or residual.  eps > 0. */
+ * fp32 values, rounded once; rstd_dev: DEVICE [n*plane].  y or sum may be x or residual.  eps > 0.  The squares are added up in fp32: where their sum is beyond its
+ * range (magnitudes near 2^64 / sqrt(c) and above), rstd is 0. */
 sk_status sknet_rms_norm(const sk_extent *extent, const sk_view *x, const sk_view *residual, const float *gamma_dev, float eps, const sk_view *sum,
                          const sk_packed *sum8, const sk_view *y, const sk_packed *y8, float *rstd_dev, void *hip_stream);
 

@@ -575,7 +575,7 @@ def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
 
 def rms_norm(x, gamma=None, eps=1e-5, axis=-1, residual=None, out=None, sum_out=None, rstd=None, y8=None, sum8=None, stream=None):
     """(y, s, rstd): y = s * rstd * gamma with s = x + residual and rstd = 1 / sqrt(mean of s^2 + eps) over the channels on `axis`.  s is x itself without a
-    residual; rstd has x's axes without the channels'.  out, sum_out, rstd: tensors to write to; out=False: no y, sum_out=False: no s (None).  y8, sum8:
+    residual (so out=x leaves no s: give sum_out or sum8 where a gradient is wanted); rstd has x's axes without the channels'.  out, sum_out, rstd: tensors to write to; out=False: no y, sum_out=False: no s (None).  y8, sum8:
     Packed that receive y and s in 8 bits (Packed.like makes one)."""
     with _Operator(x, axis, "x", stream) as op:
         if out is None:

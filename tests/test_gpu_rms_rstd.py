@@ -45,3 +45,18 @@ def test_ends_of_the_range(shape):
     _, _, rstd = B.rms_norm(x, None, eps, axis=1, out=False, sum_out=False)
     ref = 1.0 / np.sqrt(2.0 ** 126 / shape[1])
     assert (rstd[0] == 2.0 ** 70).all() and np.abs(to64(rstd[1]) / ref - 1).max() <= 1.6 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(5, 60), (5, 40000), (1, 60, 65)], ids=str)
+def test_squares_beyond_the_range(shape, kind):
+    """Finite values whose squares are not: rstd is 0, and the position alone has no digits."""
+    from paper_1509_03371_amd import binding as B
+    x = torch.ones(shape, dtype=TYPES[kind], device="cuda")
+    where = (2, 7) if len(shape) == 2 else (0, 7, 33)
+    x[where] = 2.0 ** 70
+    y, _, rstd = B.rms_norm(x, axis=1)
+    there = torch.zeros(rstd.shape, dtype=torch.bool, device="cuda")
+    there[where[0] if len(shape) == 2 else (0, 33)] = True
+    assert (rstd[there] == 0).all() and (rstd[~there] > 0.99).all()
+    assert torch.equal((y == 0).all(dim=1), there)
