@@ -36,8 +36,7 @@ struct RmsBwdArgs : NormSpan {
     PackedView s8;
     const float *rstd, *gamma;         // gamma optional
     float *dgamma;                     // optional, [c]
-    float *scratch;
-    size_t scratch_floats;
+    float *scratch;                    // rms_bwd_scratch_floats of them, if dgamma is asked for
 };
 size_t rms_bwd_scratch_floats(const NormSpan &s);
 hipError_t launch_rms_norm_bwd(const RmsBwdArgs &a, hipStream_t stream);
@@ -49,8 +48,7 @@ struct Wgrad8Args : NormSpan {         // dtype: dy's
     PackedView x;
     int accumulate;
     float *dw, *db;                    // db optional
-    float *scratch;
-    size_t scratch_floats;
+    float *scratch;                    // wgrad8_scratch_floats of them
 };
 size_t wgrad8_scratch_floats(const NormSpan &s, long c_out);
 hipError_t launch_wgrad8(const Wgrad8Args &a, hipStream_t stream);

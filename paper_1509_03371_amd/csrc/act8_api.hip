@@ -248,7 +248,6 @@ sk_status sknet_rms_norm_backward(const sk_extent *extent, const sk_view *dy, co
         a.dx = take_view(dx);
         a.rstd = rstd_dev;
         a.scratch = static_cast<float *>(workspace_dev);
-        a.scratch_floats = (size_t)(need / sizeof(float));
     }
     SK_TRY(all.settle({dy, s, dsum}));
     a.gamma = gamma_dev;
@@ -292,7 +291,6 @@ sk_status sknet_weight_gradient8(const sk_extent *extent, int64_t c_out, const s
         a.dy = take_view(dy);
         a.x = take_packed(x);
         a.scratch = static_cast<float *>(workspace_dev);
-        a.scratch_floats = (size_t)(need / sizeof(float));
     }
     SK_TRY(all.settle());
     a.c_out = c_out;

@@ -257,7 +257,7 @@ int rms_maps_bwd_copies(const NormSpan &s)
     return copies;
 }
 
-hipError_t launch_rms_maps_bwd(const RmsBwdArgs &a, int, hipStream_t stream)
+hipError_t launch_rms_maps_bwd(const RmsBwdArgs &a, hipStream_t stream)
 {
     const bool far = far_maps(a, {&a.dy, &a.s, &a.dsum, &a.dx}, {&a.s8});
     Launches done;

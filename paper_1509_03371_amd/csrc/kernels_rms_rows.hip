@@ -506,8 +506,9 @@ int rms_rows_bwd_copies(const NormSpan &s)
     return copies;
 }
 
-hipError_t launch_rms_rows_bwd(const RmsBwdArgs &a, int copies, hipStream_t stream)
+hipError_t launch_rms_rows_bwd(const RmsBwdArgs &a, hipStream_t stream)
 {
+    const int copies = rms_rows_bwd_copies(a);
     const bool in_place = a.dx.p && (a.dx.p == a.dy.p || a.dx.p == a.s.p);
     const bool far = far_apart({&a.dy, &a.s, &a.dsum, &a.dx}) || far_packed({&a.s8});
     Launches done;

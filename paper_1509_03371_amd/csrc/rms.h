@@ -40,9 +40,10 @@ hipError_t launch_rms_reduce(const float *scratch, int copies, float *dgamma, in
 
 hipError_t launch_rms_rows(const RmsArgs &a, hipStream_t stream);
 hipError_t launch_rms_maps(const RmsArgs &a, hipStream_t stream);
+// the most copies that a gradient of these sizes writes, whatever its strides
 int rms_rows_bwd_copies(const NormSpan &s);
 int rms_maps_bwd_copies(const NormSpan &s);
-hipError_t launch_rms_rows_bwd(const RmsBwdArgs &a, int copies, hipStream_t stream);
-hipError_t launch_rms_maps_bwd(const RmsBwdArgs &a, int copies, hipStream_t stream);
+hipError_t launch_rms_rows_bwd(const RmsBwdArgs &a, hipStream_t stream);
+hipError_t launch_rms_maps_bwd(const RmsBwdArgs &a, hipStream_t stream);
 
 }  // namespace sk
