@@ -6,8 +6,9 @@ namespace sk {
 namespace {
 
 // HBM bounds both.  A lane takes eight values of a line, four lanes a block, and a wave U times as many, all of them asked for before the first is used.
-// 200 x 512^2 fp32, 264 MB either way: packed in 49 us = 5.4 TB/s, unpacked in 61 = 4.3 (fp32 results are written 32 bytes a lane, in two halves; four values a lane
-// leave no gaps, and took 58 us instead of 86 alone but 75 instead of 60 behind the packing).  One thread a block: 2900 us both.
+// 200 x 512^2 fp32, 264 MB either way: packed in 49 us = 5.4 TB/s, unpacked in 61 = 4.3.  fp32 results are written 32 bytes a lane, in two halves.  Unpacking alone, over
+// and over, takes 84 us so, 68 with results stored plainly and 58 with four values a lane, which leave no gaps; but behind the packing, which leaves what it reads in the caches, 61, 77 and
+// 75: there and back 16384 x 4096 141 us, plainly 160, and 48 x 527^2 35 and 40.  One thread a block: 2900 us both.
 // LONG: a wave's values are of one line, whose place it works out on the scalar unit; a line takes as many waves as it needs.  Short lines: each lane works out
 // its own.
 template <bool LONG, int U> struct Octets {
@@ -92,6 +93,8 @@ template <int DT, int CODE, bool LONG, int U> __global__ __launch_bounds__(256) 
     }
 }
 
+// Short walks and long ones, us of packing and of unpacking 2^24 bf16 values: lines of 200 14 and 12, and 33 and 30; of 256 11 and 10, and 26 and 24; of 300 16 and 18, and 26 and 25; of 512
+// 11 and 10, and 13 and 12; of 1024 11 and 10 both.  fp32 lines of 300 and 400 pack faster in short walks (16, and 23 and 18) and unpack faster in long ones (28 and 23, and 25 and 17).
 constexpr long kLongLine = 256;
 
 // f(LONG, U, LANES), and the walk
@@ -117,11 +120,13 @@ template <class F> void pick_walk(const NormSpan &s, Walk8 &w, F f)
     typedef std::integral_constant<int, 1> One;
     typedef std::integral_constant<int, 2> Two;
     typedef std::integral_constant<int, 4> Four;
+    // (1310 x 200 2.7 us, with two octets a lane 3.4)
     const bool few = lines * octets < 64 * 1024;
     if (w.length <= 8) return few ? go(No{}, One{}, One{}) : go(No{}, Two{}, One{});
     if (w.length <= kLongLine) return few ? go(No{}, One{}, Four{}) : go(No{}, Two{}, Four{});
     // so that few pieces are left half empty
     if (octets <= 64) return go(Yes{}, One{}, Four{});
+    // (256 x 4096 2.8 us with two octets a lane, 3.7 with four; 16384 x 4096 bf16 unpacked in 33.8 and 31.5, but 2048 x 4096 fp32 packed in 8.5 and 10.2, unpacked in 11 and 16)
     if (octets <= 128 || lines * octets < 64 * 4096) return go(Yes{}, Two{}, Four{});
     return go(Yes{}, Four{}, Four{});
 }

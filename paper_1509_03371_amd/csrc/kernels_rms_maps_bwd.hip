@@ -128,8 +128,9 @@ __device__ __forceinline__ void put_gradients(const Spot<DT, P, V, FAR> &t, cons
 }
 
 // Backwards; a workgroup keeps its threads' sums for dgamma in registers over its tiles, adds them up over its pixels' lanes at the end and writes a copy of them.
-// 4 x 64 x 388^2 bf16 from int8, 193 MB in 62 us = 3.1 TB/s, and the copies' sum 4: a tile's loads, sums and stores follow one another, and the four workgroups of a CU do
-// not cover all of that.  In 16 bits 128 registers (four workgroups; some spilled) or 200 (two): 62 and 64 us; fp32 spills too many.
+// 4 x 64 x 388^2 bf16 from int8, 193 MB in 62 us = 3.1 TB/s, and the copies' sum 5: a tile's loads, sums and stores follow one another, and the four workgroups of a CU do
+// not cover all of that.  In 16 bits 128 registers (four workgroups; some spilled) or 200 (two): 62 and 64 us; fp32 spills too many.  With the copies' sum: from a tensor 62 us = 3.8
+// TB/s, fp32 100 = 4.6, from int8 85 = 4.1.  (The next tile's loads at 200 registers: not tried.)
 template <int DT, int P, int V, int K, int T, bool HELD> __global__ __launch_bounds__(T, DT == 0 ? 2 : 4) void rms_maps_bwd_kernel(RmsBwdArgs a, long tiles, long tiles_of_image)
 {
     __shared__ float part[T > 64 ? 2 * (T / 64) * P * V : 1];

@@ -46,7 +46,7 @@ template <int DT, int G> __device__ __forceinline__ void put_row(const Row<DT, G
 }
 
 // G lanes hold a row, K octets each: one read and one write.  Squares need no mean taken off, so the sum of them is the one sum there is.  HBM bounds it: residual,
-// sum and e4m3 result of 16384 x 4096 bf16, 471 MB in 84 us = 5.6 TB/s; 16 x 1024 bf16 3.6 us, a launch.
+// sum and e4m3 result of 16384 x 4096 bf16, 471 MB in 84 us = 5.6 TB/s; 16 x 1024 bf16 3.8 us, a launch.
 template <int DT, int G, int K, int T> __global__ __launch_bounds__(T) void rms_rows_kernel(RmsArgs a)
 {
     __shared__ float part[G > 64 ? 2 * (G / 64) : 1];
@@ -210,7 +210,7 @@ template <int DT, int T, bool HELD> __device__ void rms_rows_sums(const RmsBwdAr
 
 // Backwards: a workgroup takes R = T / G rows at a time, gridDim.x * R apart, and keeps its lanes' sums for dgamma in registers until the end, where they are added
 // up over the R rows' lanes through LDS and go to the workgroup's copy of the scratch, or to dgamma itself if there is one workgroup.  16384 x 4096 bf16 from a
-// sum in e4m3, with dsum: 472 MB in 88 us = 5.4 TB/s, and the copies' sum 4.4.
+// sum in e4m3, with dsum: 472 MB in 89 us = 5.3 TB/s, and the copies' sum 4.8.
 //
 // ROLES, for few rows: the first `walkers` workgroups leave the sums alone, and each of the others takes them for 64 channels over all rows, which are read twice
 // (from the L2): one launch and no workspace.
@@ -375,7 +375,8 @@ template <int DT, bool HELD> __global__ __launch_bounds__(1024) void rms_long_ro
     }
 }
 
-// dgamma of rows too long for registers: a thread eight channels, blockIdx.y a share of the rows
+// dgamma of rows too long for registers: a thread eight channels, blockIdx.y a share of the rows.  At most sixteen shares, few workgroups: 8192 x 16392 bf16 365 us of the gradient's
+// 932 (rows of 16384, which fit: 155 in all).
 template <int DT, bool HELD> __global__ __launch_bounds__(1024) void rms_long_rows_dgamma_kernel(RmsBwdArgs a)
 {
     const Row<DT, 1024> r(a.c);
@@ -491,7 +492,9 @@ hipError_t launch_rms_rows(const RmsArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Where ROLES take the work: few rows, as the layer norm's gradient (whose figures for both ways these kernels share).  37 x 777 fp32: 4.3 us.
+// Where ROLES take the work: up to 512 rows, 1024 of more than 2048 channels.  With roles and with copies and a second launch, us, bf16 (fp32): 37 x 777 4.2 and 7.0 (3.8 and 6.8),
+// 512 x 777 6.3 and 7.4 (7.2 and 7.2), 768 x 777 7.9 and 7.7 (10.6 and 7.6); 512 x 2048 4.7 and 7.6 (6.7 and 8.2), 1024 x 2048 10.0 and 9.2 (14 and 12); 512 x 4096 7.1 and 10.8 (10.8 and
+// 13.9), 1024 x 4096 12.7 and 17.0 (17.8 and 17.0), 2048 x 4096 23 and 17 (30 and 24).
 static bool takes_roles(const NormSpan &s) { return s.c > 8 && s.c <= kLongRowBwd && s.n <= (s.c > 2048 ? 1024 : 512); }
 
 int rms_rows_bwd_copies(const NormSpan &s)

@@ -44,7 +44,10 @@ Plan8 plan_of(const NormSpan &s, long c_out)
         p.splits = std::min(most, std::max<long>(1, fill / tiles));
         return tiles * p.splits;
     };
-    // as many workgroups as fill the card: one a CU of big ones (bf16 takes small ones, see the kernel), else two
+    // As many workgroups as fill the card: one a CU of big ones (bf16 takes small ones, see the kernel), else two.  Big ones where they fill half the card or more with
+    // four copies of the gradient at most.  us with big and with small ones, fp16 (fp32): 2048 x 2048 weights over 8192 rows 184 and 219 (247 and 310), over 4096 120 and 134 (150 and
+    // 181), over 1024 72 and 73 (80 and 83); with more copies 512 x 1024 over 128^2 pixels 59 and 60 (81 and 84), 512 x 512 over 65536 rows 91 and 102 (123 and 154), 256 x 256 over as
+    // many 43 and 38 (52 and 50).  The rule leaves up to a quarter there; and over 300 rows, a few steps, small ones would take 20 of its 66 us.
     if (s.dtype != 1 && c_out >= 256 && s.c >= 256 && lay(256, 256, true, 256) >= 128 && p.splits <= 4) return p;
     const int tm = c_out <= 64 ? 64 : 128, tn = s.c <= 64 ? 64 : 128;
     // (three a CU where the tile is small: 200 x 48 weights over 512^2 pixels 42 us with two and 39 with three; 512 x 1024 over 128^2 62 and 78)
@@ -194,10 +197,12 @@ template <bool IS_ROWS> __device__ __forceinline__ bf16x8 fragment(const char *l
 
 // A workgroup takes TM x TN weights and a share of the positions, KS at a time: its threads load 32 values of a line each (of x a block with its scale), a step
 // ahead, widen them on their way into LDS, and its waves multiply, a part of the tile each.  db comes out of the same fragments, times ones.
-// 16384 rows, 2048 x 4096 weights, 275 GFLOP: bf16 and e4m3 350 us = 0.79 PFLOP/s, int8 396 (a library product of bf16 tensors 231: 1.19).  Waves that multiply go first
-// (s_setprio): 398 without.  What is left waits for the loads of a step, of which one is under way: three workgroups a CU at 160 registers cover for one another, two (240
-// registers) take 483 us, steps of 32 positions 464, 256 x 128 tiles of four waves with two steps under way 668.  fp16 and fp32 have two and three products for each
-// load, and there BIG tiles pay: 8192 rows, 2048 x 2048 fp16 184 us and 253 with small ones (bf16 424 and 398).
+// 16384 rows, 2048 x 4096 weights, 275 GFLOP: bf16 and e4m3 349 us = 0.79 PFLOP/s, int8 395 (a library product of bf16 tensors 231: 1.19), passes one after another; the
+// first hundred or so after a pause take up to 430.  Waves that multiply go first (s_setprio): 398 without.  Of a CU's clocks the matrix units work in 31 of 100 and the LDS in 46 (for 32
+// positions of a tile it moves 48 KB, one and a half times as long as the products take, a third of it banks in conflict); the rest waits, for the loads of a step, of
+// which one is under way, for one another and for the LDS.  Three workgroups a CU at 160 registers cover for one another, two (240 registers) take 483 us, steps of 32 positions
+// 464, 256 x 128 tiles of four waves with two steps under way 668.  fp16 and fp32 have two and three products for each load, and there BIG tiles pay: fp16 608 us and 655
+// with small ones (bf16 422 and 349).
 template <int DT, int CODE, bool IS_ROWS, int TM, int TN, bool BIG> __global__ __launch_bounds__(BIG ? 512 : 256, 2) void wgrad8_kernel(Wgrad8Launch a)
 {
     constexpr int NS = terms<DT>, B = DT == 0 ? 4 : 2, T = BIG ? 512 : 256, KS = step_of<DT, BIG>;
